@@ -217,12 +217,12 @@ def run(s):
     from paper_1610_06209_amd import binding as sp
     kind = s["kind"]
     if kind == "quantise":
-        codes, scales = sp.spinner_mx4_quantize(s["x"])
-        return sp.spinner_mx4_dequantize(codes, scales, TYPES[s["out"]])
+        codes, scales = sp.spinner_mx_quantize(s["x"])
+        return sp.spinner_mx_dequantize(codes, scales, TYPES[s["out"]])
     if kind == "product":
-        return sp.spinner_mx4_matmul(s["a_codes"], s["a_scales"], s["w_codes"], s["w_scales"], dtype=TYPES[s["out"]])
+        return sp.spinner_mx_matmul(s["a_codes"], s["a_scales"], s["w_codes"], s["w_scales"], dtype=TYPES[s["out"]])
     if kind == "linear":
-        return sp.spinner_mx4_linear(s["x"], s["w_codes"], s["w_scales"], s["diag"], s["block"], s.get("ends"))
+        return sp.spinner_mx_linear(s["x"], s["w_codes"], s["w_scales"], s["diag"], s["block"], s.get("ends"))
     y = sp.spinner_grouped_matmul(s["x"], s["w"], s["ends"])
     if kind == "grouped":
         return y
