@@ -48,7 +48,9 @@ enum {
     SPINNER_ERR_BAD_L        = -8,  /* L < 1                                                */
     SPINNER_ERR_ALIGNMENT    = -9,  /* a data pointer is not 16-byte aligned                */
     SPINNER_ERR_UNSUPPORTED  = -10, /* combination not built (e.g. hashing with n > 2^16)   */
-    SPINNER_ERR_SCRATCH_LIMIT = -11 /* needs more scratch than the built-in buffer of an allocation-free entry point */
+    SPINNER_ERR_SCRATCH_LIMIT = -11, /* needs more scratch than the built-in buffer of an allocation-free entry point */
+    SPINNER_ERR_BAD_TYPE     = -12, /* an element type that the entry point does not take   */
+    SPINNER_ERR_BAD_SHAPE    = -13  /* a size, stride, number of experts or run of coordinates outside the stated range */
 };
 
 typedef enum {
@@ -389,6 +391,108 @@ size_t spinner_struct_workspace_bytes(int kind, int n, long batch);
 int spinner_struct_apply_ws(const float *x, int n, long batch, int kind, const void *spectrum,
                             const float *d1, const float *d2, int m, float scale,
                             float *out, void *workspace, void *stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Linear layers on rotated vectors: microscaled 4-bit numbers, and products of
+ * rows that are grouped by expert
+ * ---------------------------------------------------------------------------
+ * The rotation H D spreads a vector's large coordinates over all of them
+ * (balancedness, Remark 1), which is what lets a layer's inputs and weights go
+ * into 4 bits.  Rotating both operands of a product leaves the product as it
+ * is: (H D x) . (H D w) = x . w.
+ *
+ * Format: 32 neighbours of a row share a scale.  codes is uint8 [rows][k / 2],
+ * coordinate 2i in the low half of byte i; a code is e2m1: sign, two bits of
+ * exponent, one of mantissa, values 0, 0.5, 1, 1.5, 2, 3, 4, 6.  scales is
+ * uint8 [rows][k / 32]: 2^(byte - 127), 255 stands for NaN (every number of
+ * its 32 then is NaN, and so is every product with them).
+ *
+ * Element types of tensors of plain numbers; sums are fp32 throughout.
+ */
+typedef enum { SPINNER_F32 = 0, SPINNER_BF16 = 1, SPINNER_F16 = 2 } spinner_dtype_t;
+
+/*
+ * Rotate and quantise.  On each run of `block` coordinates v = H D x (H the
+ * normalised Hadamard matrix of that size, D = diag(d)); block = 0: v = x.  For
+ * every 32 of them, with a = max |v|: scale 2^e, e = floor(log2 a) - 2 held at
+ * -127 and above, codes v / 2^e rounded to the nearest, ties to even, and held
+ * at +-6.  All zeros: byte 0.  An infinity or a NaN among the 32: byte 255,
+ * codes 0 (with a rotation, all of its run).
+ *
+ *   x         in   device [rows][k] of type dtype, rows x_stride elements apart
+ *                  (any stride >= 0, so that a row may be repeated)
+ *   rows      in   0 <= rows < 2^31
+ *   k         in   a multiple of 32, up to 2^24
+ *   diag      in   device fp32 [k], or NULL for D = I
+ *   block     in   0, or a power of two in [32, 4096] that divides k
+ *   codes     out  device uint8 [rows][k / 2]
+ *   scales    out  device uint8 [rows][k / 32], of any alignment
+ */
+int spinner_mx_quantize(const void *x, int dtype, long rows, int k, long x_stride,
+                         const float *diag, int block,
+                         void *codes, void *scales, void *stream);
+
+/* The numbers that codes stand for, to out [rows][k] of type dtype, rows out_stride >= k elements apart. */
+int spinner_mx_dequantize(const void *codes, const void *scales, long rows, int k,
+                           void *out, int dtype, long out_stride, void *stream);
+
+/*
+ * out[r][j] = sum_i a[r][i] w[e][j][i] on 4-bit operands (the fp4 matrix pipe):
+ * products are exact, sums fp32, one rounding to the type of out.
+ *
+ *   a_codes, a_scales  in   device, [rows][k] in the format above
+ *   w_codes, w_scales  in   device, [experts][n][k]
+ *   n                  in   1 <= n <= 2^24
+ *   experts            in   1 <= experts <= 1024
+ *   ends               in   device int64 [experts]: the rows of expert e are
+ *                           those from ends[e - 1] (0 for the first) up to but
+ *                           without ends[e].  NULL with experts = 1: all rows.
+ *   out                out  device [rows][n] of type dtype, out_stride >= n
+ *                           elements from row to row
+ *
+ * An expert may have no rows.  Rows from the last end on belong to none and come
+ * out as 0.  ends is read on the GPU only, and held between 0 and rows and to
+ * rise there, whatever it contains.
+ */
+int spinner_mx_matmul(const void *a_codes, const void *a_scales, long rows, int k,
+                       const void *w_codes, const void *w_scales, int n,
+                       int experts, const long long *ends,
+                       void *out, int dtype, long out_stride, void *stream);
+
+/*
+ * spinner_mx_quantize and spinner_mx_matmul in one call, out of the type of x:
+ * a layer with 4-bit weights (quantised with the same diag and block) on plain
+ * inputs.  workspace: spinner_mx_linear_workspace_bytes(rows, k) bytes.
+ */
+size_t spinner_mx_linear_workspace_bytes(long rows, int k);
+int spinner_mx_linear(const void *x, int dtype, long rows, int k, long x_stride,
+                       const float *diag, int block,
+                       const void *w_codes, const void *w_scales, int n,
+                       int experts, const long long *ends,
+                       void *out, long out_stride, void *workspace, void *stream);
+
+/*
+ * The same grouped products on 16-bit operands (dtype SPINNER_BF16 or
+ * SPINNER_F16), and the two gradients of a training step:
+ *     spinner_grouped_matmul     out[r][j]   = sum_i x[r][i]  w[e][j][i]
+ *     spinner_grouped_matmul_dx  dx[r][i]    = sum_j dy[r][j] w[e][j][i]
+ *     spinner_grouped_matmul_dw  dw[e][j][i] = sum_r dy[r][j] x[r][i]   over the rows of expert e
+ * with w device [experts][n][k].  k and n may be anything up to 2^24; rows that
+ * are made of whole 16-byte pieces (k, n and the strides multiples of 8) take
+ * the faster way.  dw is overwritten, zeros for an expert without rows, in fp32
+ * or in the type of dy and x (dw_dtype).  Rows of no expert: 0 in out and dx,
+ * and not in dw.  Strides as above.
+ */
+int spinner_grouped_matmul(const void *x, int dtype, long rows, int k, long x_stride,
+                           const void *w, int n, int experts, const long long *ends,
+                           void *out, long out_stride, void *stream);
+int spinner_grouped_matmul_dx(const void *dy, int dtype, long rows, int n, long dy_stride,
+                              const void *w, int k, int experts, const long long *ends,
+                              void *dx, long dx_stride, void *stream);
+int spinner_grouped_matmul_dw(const void *dy, const void *x, int dtype, long rows, int n, int k,
+                              long dy_stride, long x_stride, int experts, const long long *ends,
+                              void *dw, int dw_dtype, void *stream);
 
 /*
  * Bytes of device scratch spinner_apply needs for these arguments: 0 up to the

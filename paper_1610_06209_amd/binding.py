@@ -26,6 +26,8 @@ SPINNER_ERR_BAD_L = -8
 SPINNER_ERR_ALIGNMENT = -9
 SPINNER_ERR_UNSUPPORTED = -10
 SPINNER_ERR_SCRATCH_LIMIT = -11
+SPINNER_ERR_BAD_TYPE = -12
+SPINNER_ERR_BAD_SHAPE = -13
 
 SPINNER_EPI_NONE = 0
 SPINNER_EPI_COSSIN = 1
@@ -40,7 +42,9 @@ EXPORTS = ["spinner_apply", "spinner_hash", "spinner_workspace_bytes", "spinner_
            "spinner_sketch_gram_workspace_bytes", "spinner_sketch_gram_static", "spinner_sketch_gram_static_limit",
            "spinner_blocks_workspace_bytes", "spinner_apply_blocks",
            "spinner_struct_params", "spinner_struct_spectrum_bytes", "spinner_struct_prepare", "spinner_struct_apply",
-           "spinner_struct_workspace_bytes", "spinner_struct_apply_ws"]
+           "spinner_struct_workspace_bytes", "spinner_struct_apply_ws",
+           "spinner_mx_quantize", "spinner_mx_dequantize", "spinner_mx_matmul", "spinner_mx_linear_workspace_bytes",
+           "spinner_mx_linear", "spinner_grouped_matmul", "spinner_grouped_matmul_dx", "spinner_grouped_matmul_dw"]
 
 if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_native.so")):
     raise ImportError(
@@ -138,6 +142,23 @@ lib.spinner_struct_apply_ws.argtypes = [_vp, ctypes.c_int, ctypes.c_long, ctypes
 lib.spinner_struct_apply.restype = ctypes.c_int
 lib.spinner_struct_apply.argtypes = [_vp, ctypes.c_int, ctypes.c_long, ctypes.c_int, _vp, _vp, _vp, ctypes.c_int, ctypes.c_float,
                                      _vp, _vp]
+_int, _long = ctypes.c_int, ctypes.c_long
+lib.spinner_mx_quantize.restype = _int
+lib.spinner_mx_quantize.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _vp, _vp, _vp]
+lib.spinner_mx_dequantize.restype = _int
+lib.spinner_mx_dequantize.argtypes = [_vp, _vp, _long, _int, _vp, _int, _long, _vp]
+lib.spinner_mx_matmul.restype = _int
+lib.spinner_mx_matmul.argtypes = [_vp, _vp, _long, _int, _vp, _vp, _int, _int, _vp, _vp, _int, _long, _vp]
+lib.spinner_mx_linear_workspace_bytes.restype = ctypes.c_size_t
+lib.spinner_mx_linear_workspace_bytes.argtypes = [_long, _int]
+lib.spinner_mx_linear.restype = _int
+lib.spinner_mx_linear.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _vp, _vp, _int, _int, _vp, _vp, _long, _vp, _vp]
+lib.spinner_grouped_matmul.restype = _int
+lib.spinner_grouped_matmul.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _int, _vp, _vp, _long, _vp]
+lib.spinner_grouped_matmul_dx.restype = _int
+lib.spinner_grouped_matmul_dx.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _int, _vp, _vp, _long, _vp]
+lib.spinner_grouped_matmul_dw.restype = _int
+lib.spinner_grouped_matmul_dw.argtypes = [_vp, _vp, _int, _long, _int, _int, _long, _long, _int, _vp, _vp, _int, _vp]
 STRUCT_KINDS = {"circulant": 0, "skew_circulant": 1, "toeplitz": 2, "hankel": 3}
 
 
@@ -784,3 +805,249 @@ def spinner_struct_apply_ws(x, kind, spectrum, d1, d2, m=None, scale=1.0, out=No
     if rc != SPINNER_OK:
         raise SpinnerError(rc)
     return out
+
+
+# ------------------------------------------------------------------ 4-bit numbers and products of rows grouped by expert
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MX4_BLOCK = 32
+
+
+def _dtype_code(dtype):
+    if dtype not in DTYPES:
+        raise SpinnerError(SPINNER_ERR_BAD_TYPE)
+    return DTYPES[dtype]
+
+
+def _check_here(t, name, dtype=None, dim=None):
+    """A tensor of the expected type and number of dimensions on the GPU that the call runs on."""
+    if not t.is_cuda or (dtype is not None and t.dtype != dtype) or (dim is not None and t.dim() != dim):
+        raise ValueError("%s must be a %s%sCUDA tensor" % (name, "" if dim is None else "%d-dimensional " % dim,
+                                                         "" if dtype is None else "%s " % dtype))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current GPU" % name)
+
+
+def _check_bytes(t, name, shape):
+    _check_here(t, name, torch.uint8)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous, of shape %s" % (name, tuple(shape)))
+
+
+def _check_rows(t, name, dtype=None):
+    """[rows][numbers], numbers side by side; returns the distance between rows."""
+    _check_here(t, name, dtype, 2)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("the numbers of a row of %s must lie side by side" % name)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _new_or_checked(out, name, shape, dtype, like):
+    """A result of rows (the caller's may have rows further apart) and the distance between them."""
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=like.device)
+    stride = _check_rows(out, name, dtype)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError("%s has the wrong size" % name)
+    if stride < shape[1]:
+        raise ValueError("rows of %s lie over one another" % name)
+    return out, stride
+
+
+def _check_ends(ends, experts, weights):
+    """The ends of the experts' rows; None goes with a single weight matrix."""
+    if ends is None:
+        if experts != 1:
+            raise ValueError("ends is needed: %s holds %d experts" % (weights, experts))
+        return None
+    _check_here(ends, "ends", torch.int64, 1)
+    if ends.numel() != experts or not ends.is_contiguous():
+        raise ValueError("ends must be contiguous, one number for each of %d experts" % experts)
+    return ends.data_ptr()
+
+
+def _check_weights(w, name):
+    """[n][k] or [experts][n][k], contiguous; returns experts, n, k."""
+    _check_here(w, name)
+    if w.dim() not in (2, 3) or not w.is_contiguous():
+        raise ValueError("%s must be a contiguous [n][k] or [experts][n][k] CUDA tensor" % name)
+    return (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
+
+
+def _check_rotation(diag, block, k):
+    if diag is None:
+        return None
+    _check_here(diag, "diag", torch.float32, 1)
+    if diag.numel() != k or not diag.is_contiguous():
+        raise ValueError("diag must be contiguous, one number for each of %d coordinates" % k)
+    return diag.data_ptr()
+
+
+def _in_use(stream, *tensors):
+    """Tensors made here that an explicit stream works on: their memory is not given away before it has."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _done(rc):
+    if rc != SPINNER_OK:
+        raise SpinnerError(rc)
+
+
+def spinner_mx_quantize(x, diag=None, block=0, codes=None, scales=None, stream=None):
+    """Rotate runs of ``block`` coordinates (v = H D x, D = diag(diag); block = 0: v = x) and round to microscaled 4-bit numbers.
+
+    x: fp32, bf16 or fp16 CUDA tensor [rows][k], rows any distance apart, k a multiple of 32.  diag: fp32 [k] or None (D = I).
+    Returns (codes uint8 [rows][k / 2], scales uint8 [rows][k / 32]); see include/spinner.h for the format.
+    """
+    r = _native.mx_quantize(x, diag, block, codes, scales, stream)
+    if r is not None:
+        return r
+    stride = _check_rows(x, "x")
+    rows, k = x.shape
+    given = codes is not None, scales is not None
+    if codes is None:
+        codes = torch.empty((rows, k // 2), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((rows, k // MX4_BLOCK), dtype=torch.uint8, device=x.device)
+    _check_bytes(codes, "codes", (rows, k // 2))
+    _check_bytes(scales, "scales", (rows, k // MX4_BLOCK))
+    d = _check_rotation(diag, block, k)
+    _done(lib.spinner_mx_quantize(x.data_ptr(), _dtype_code(x.dtype), rows, k, stride, d, int(block), codes.data_ptr(), scales.data_ptr(),
+                                   _stream_handle(stream)))
+    _in_use(stream, None if given[0] else codes, None if given[1] else scales)
+    return codes, scales
+
+
+def spinner_mx_dequantize(codes, scales, dtype=torch.float32, out=None, stream=None):
+    """The numbers that 4-bit codes stand for: [rows][k] of ``dtype``."""
+    r = _native.mx_dequantize(codes, scales, dtype, out, stream)
+    if r is not None:
+        return r
+    _check_here(codes, "codes", torch.uint8, 2)
+    rows, k = codes.shape[0], 2 * codes.shape[1]
+    _check_bytes(codes, "codes", (rows, k // 2))
+    _check_bytes(scales, "scales", (rows, k // MX4_BLOCK))
+    code = _dtype_code(dtype)
+    made = out is None
+    out, stride = _new_or_checked(out, "out", (rows, k), dtype, codes)
+    _done(lib.spinner_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, out.data_ptr(), code, stride, _stream_handle(stream)))
+    _in_use(stream, out if made else None)
+    return out
+
+
+def spinner_mx_matmul(a_codes, a_scales, w_codes, w_scales, ends=None, dtype=torch.bfloat16, out=None, stream=None):
+    """out = a w^T on 4-bit operands: a [rows][k], w [n][k], or [experts][n][k] with each expert's rows up to its entry of ``ends``.
+
+    codes and scales as spinner_mx_quantize gives them (w's with the experts in front); ends: int64 CUDA tensor [experts],
+    cumulative.  Rows from the last end on come out as 0.
+    """
+    r = _native.mx_matmul(a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream)
+    if r is not None:
+        return r
+    _check_here(a_codes, "a_codes", torch.uint8, 2)
+    rows, k = a_codes.shape[0], 2 * a_codes.shape[1]
+    _check_bytes(a_codes, "a_codes", (rows, k // 2))
+    _check_bytes(a_scales, "a_scales", (rows, k // MX4_BLOCK))
+    experts, n, _ = _check_weights(w_codes, "w_codes")
+    _check_bytes(w_codes, "w_codes", (*w_codes.shape[:-1], k // 2))
+    _check_bytes(w_scales, "w_scales", (*w_codes.shape[:-1], k // MX4_BLOCK))
+    e = _check_ends(ends, experts, "w_codes")
+    code = _dtype_code(dtype)
+    made = out is None
+    out, stride = _new_or_checked(out, "out", (rows, n), dtype, a_codes)
+    _done(lib.spinner_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), rows, k, w_codes.data_ptr(), w_scales.data_ptr(), n, experts, e,
+                                 out.data_ptr(), code, stride, _stream_handle(stream)))
+    _in_use(stream, out if made else None)
+    return out
+
+
+def spinner_mx_linear_workspace_bytes(rows: int, k: int) -> int:
+    return int(lib.spinner_mx_linear_workspace_bytes(int(rows), int(k)))
+
+
+def spinner_mx_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, out=None, workspace=None, stream=None):
+    """A layer with 4-bit weights on plain inputs: spinner_mx_quantize(x, diag, block), then spinner_mx_matmul; out of the type of x.
+
+    The weights are quantised with the same diag and block, which then cancel in the product.
+    """
+    r = _native.mx_linear(x, w_codes, w_scales, diag, block, ends, out, workspace, stream)
+    if r is not None:
+        return r
+    x_stride = _check_rows(x, "x")
+    code = _dtype_code(x.dtype)
+    rows, k = x.shape
+    experts, n, _ = _check_weights(w_codes, "w_codes")
+    _check_bytes(w_codes, "w_codes", (*w_codes.shape[:-1], k // 2))
+    _check_bytes(w_scales, "w_scales", (*w_codes.shape[:-1], k // MX4_BLOCK))
+    d = _check_rotation(diag, block, k)
+    e = _check_ends(ends, experts, "w_codes")
+    made = out is None, workspace is None
+    out, stride = _new_or_checked(out, "out", (rows, n), x.dtype, x)
+    need = spinner_mx_linear_workspace_bytes(rows, k)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check_workspace(workspace, need)
+    _done(lib.spinner_mx_linear(x.data_ptr(), code, rows, k, x_stride, d, int(block), w_codes.data_ptr(), w_scales.data_ptr(), n, experts, e,
+                                 out.data_ptr(), stride, workspace.data_ptr(), _stream_handle(stream)))
+    _in_use(stream, out if made[0] else None, workspace if made[1] else None)
+    return out
+
+
+def _grouped(call, a, w, ends, out, stream, across):
+    a_stride = _check_rows(a, "x" if across else "dy")
+    code = _dtype_code(a.dtype)
+    experts, n, k = _check_weights(w, "w")
+    if w.dtype != a.dtype or a.shape[1] != (k if across else n):
+        raise ValueError("w must be of the type and width of the rows")
+    e = _check_ends(ends, experts, "w")
+    made = out is None
+    out, stride = _new_or_checked(out, "out" if across else "dx", (a.shape[0], n if across else k), a.dtype, a)
+    depth, width = (k, n) if across else (n, k)
+    _done(call(a.data_ptr(), code, a.shape[0], depth, a_stride, w.data_ptr(), width, experts, e, out.data_ptr(), stride, _stream_handle(stream)))
+    _in_use(stream, out if made else None)
+    return out
+
+
+def spinner_grouped_matmul(x, w, ends=None, out=None, stream=None):
+    """out = x w^T of each expert's rows with its own weights: x bf16 or fp16 [rows][k], w [experts][n][k] (or [n][k] without ends).
+
+    ends: int64 CUDA tensor [experts]; the rows of expert e are ends[e - 1] .. ends[e].  Rows from the last end on come out as 0.
+    """
+    r = _native.grouped_matmul(x, w, ends, out, stream)
+    return r if r is not None else _grouped(lib.spinner_grouped_matmul, x, w, ends, out, stream, True)
+
+
+def spinner_grouped_matmul_dx(dy, w, ends=None, dx=None, stream=None):
+    """Gradient of spinner_grouped_matmul with respect to x: dx = dy w of each expert's rows."""
+    r = _native.grouped_matmul_dx(dy, w, ends, dx, stream)
+    return r if r is not None else _grouped(lib.spinner_grouped_matmul_dx, dy, w, ends, dx, stream, False)
+
+
+def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, stream=None):
+    """Gradient with respect to w: dw = dy^T x over each expert's rows, [experts][n][k] ([n][k] without ends).
+
+    dtype: fp32, or the type of dy and x.  Experts without rows get zeros.
+    """
+    r = _native.grouped_matmul_dw(dy, x, ends, dtype, dw, stream)
+    if r is not None:
+        return r
+    dy_stride, x_stride = _check_rows(dy, "dy"), _check_rows(x, "x", dy.dtype)
+    code, dw_code = _dtype_code(dy.dtype), _dtype_code(dtype)
+    rows, n, k = dy.shape[0], dy.shape[1], x.shape[1]
+    if x.shape[0] != rows:
+        raise ValueError("dy and x must have as many rows")
+    experts = 1 if ends is None else ends.numel()
+    e = _check_ends(ends, experts, "dw")
+    shape = (n, k) if ends is None else (experts, n, k)
+    made = dw is None
+    if made:
+        dw = torch.empty(shape, dtype=dtype, device=dy.device)
+    _check_here(dw, "dw", dtype)
+    if tuple(dw.shape) != shape or not dw.is_contiguous():
+        raise ValueError("dw must be contiguous, of shape %s" % (shape,))
+    _done(lib.spinner_grouped_matmul_dw(dy.data_ptr(), x.data_ptr(), code, rows, n, k, dy_stride, x_stride, experts, e, dw.data_ptr(), dw_code,
+                                        _stream_handle(stream)))
+    _in_use(stream, dw if made else None)
+    return dw

@@ -10,6 +10,7 @@
 
 #include "launch.hpp"
 #include "layer_params.hpp"
+#include "mx4.hpp"
 
 namespace spinner {
 // ------------------------------------------------------------------ plain copy (measurement aid)
@@ -92,6 +93,8 @@ const char* spinner_strerror(int status)
     case SPINNER_ERR_ALIGNMENT: return "data pointers must be 16-byte aligned";
     case SPINNER_ERR_UNSUPPORTED: return "combination not supported";
     case SPINNER_ERR_SCRATCH_LIMIT: return "problem needs more scratch than the library's built-in buffer holds";
+    case SPINNER_ERR_BAD_TYPE: return "element type not taken here";
+    case SPINNER_ERR_BAD_SHAPE: return "a size, a stride, the number of experts or the run of coordinates is outside its range";
     default: return "unknown status";
     }
 }
@@ -875,6 +878,187 @@ int spinner_stream_copy(const float* src, float* dst, size_t count, void* stream
                        reinterpret_cast<float4*>(dst), count4);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPINNER_OK : hip_fail(e);
+}
+
+// ------------------------------------------------------------------ 4-bit numbers and grouped products
+static_assert(SPINNER_F32 == spinner::kF32 && SPINNER_BF16 == spinner::kBf16 && SPINNER_F16 == spinner::kF16, "the element types");
+
+static bool plain_type(int dtype) { return dtype == SPINNER_F32 || dtype == SPINNER_BF16 || dtype == SPINNER_F16; }
+static bool type16(int dtype) { return dtype == SPINNER_BF16 || dtype == SPINNER_F16; }
+static bool side(int n) { return n >= 1 && n <= (1 << 24); }
+static bool mx4_depth(int k) { return side(k) && k % spinner::kMx4Block == 0; }
+// strides in elements: 64-bit byte offsets hold rows * stride
+static bool stride_in(long stride) { return stride >= 0 && stride <= (1L << 30); }
+static bool stride_out(long stride, int width, long rows) { return rows <= 1 ? stride >= 0 : stride >= width && stride <= (1L << 30); }
+
+static int launched(hipError_t e)
+{
+    if (e == hipErrorInvalidConfiguration) return SPINNER_ERR_BAD_BATCH;      // more workgroups than a grid holds
+    return e == hipSuccess ? SPINNER_OK : hip_fail(e);
+}
+
+static int check_quantize(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    if (rows < 0 || rows > 0x7fffffffL) return SPINNER_ERR_BAD_BATCH;
+    if (!mx4_depth(k) || !stride_in(x_stride)) return SPINNER_ERR_BAD_SHAPE;
+    if (block && (block < 32 || block > spinner::kMaxRotation || (block & (block - 1)) || k % block)) return SPINNER_ERR_BAD_SHAPE;
+    if (diag && !block) return SPINNER_ERR_BAD_SHAPE;
+    if (rows && !x) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(x) || !aligned16(diag)) return SPINNER_ERR_ALIGNMENT;
+    return SPINNER_OK;
+}
+
+int spinner_mx_quantize(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block, void* codes,
+                         void* scales, void* stream)
+{
+    const int rc = check_quantize(x, dtype, rows, k, x_stride, diag, block);
+    if (rc != SPINNER_OK) return rc;
+    if (rows == 0) return SPINNER_OK;
+    if (!codes || !scales) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(codes)) return SPINNER_ERR_ALIGNMENT;
+    spinner::QuantizeParams p = {x, diag, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), x_stride, (int)rows, k};
+    return launched(spinner::launch_mx4_quantize(p, dtype, block, static_cast<hipStream_t>(stream)));
+}
+
+int spinner_mx_dequantize(const void* codes, const void* scales, long rows, int k, void* out, int dtype, long out_stride, void* stream)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    if (rows < 0 || rows > 0x7fffffffL) return SPINNER_ERR_BAD_BATCH;
+    if (!mx4_depth(k) || !stride_out(out_stride, k, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!codes || !scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(codes) || !aligned16(out)) return SPINNER_ERR_ALIGNMENT;
+    return launched(spinner::launch_mx4_dequantize(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), (int)rows, k,
+                                                   out, dtype, out_stride, static_cast<hipStream_t>(stream)));
+}
+
+// rows, experts and their ends
+static int check_groups(long rows, int experts, const long long* ends)
+{
+    if (rows < 0 || rows > 0x7fffffffL) return SPINNER_ERR_BAD_BATCH;
+    if (experts < 1 || experts > spinner::kMaxExperts) return SPINNER_ERR_BAD_SHAPE;
+    if (experts > 1 && !ends) return SPINNER_ERR_NULL_PTR;
+    if (reinterpret_cast<uintptr_t>(ends) & 7u) return SPINNER_ERR_ALIGNMENT;
+    return SPINNER_OK;
+}
+
+int spinner_mx_matmul(const void* a_codes, const void* a_scales, long rows, int k, const void* w_codes, const void* w_scales, int n,
+                       int experts, const long long* ends, void* out, int dtype, long out_stride, void* stream)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    const int rc = check_groups(rows, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    if (!mx4_depth(k) || !side(n) || !stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(a_codes) || !aligned16(w_codes) || !aligned16(out)) return SPINNER_ERR_ALIGNMENT;
+    spinner::ProductParams p = {};
+    p.a = static_cast<const char*>(a_codes);
+    p.b = static_cast<const char*>(w_codes);
+    p.a_scales = static_cast<const uint8_t*>(a_scales);
+    p.b_scales = static_cast<const uint8_t*>(w_scales);
+    p.out = static_cast<char*>(out);
+    p.ends = ends;
+    p.a_stride = p.b_stride = k / 2;
+    p.b_group = (long long)n * (k / 2);
+    p.out_stride = out_stride;
+    p.rows = (int)rows;
+    p.experts = experts;
+    p.width = n;
+    p.depth = k;
+    return launched(spinner::launch_product_mx4(dtype, p, static_cast<hipStream_t>(stream)));
+}
+
+size_t spinner_mx_linear_workspace_bytes(long rows, int k)
+{
+    if (rows < 0 || rows > 0x7fffffffL || !mx4_depth(k)) return 0;
+    return (size_t)rows * (k / 2 + k / spinner::kMx4Block);
+}
+
+int spinner_mx_linear(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block, const void* w_codes,
+                       const void* w_scales, int n, int experts, const long long* ends, void* out, long out_stride, void* workspace,
+                       void* stream)
+{
+    int rc = check_quantize(x, dtype, rows, k, x_stride, diag, block);
+    if (rc == SPINNER_OK) rc = check_groups(rows, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    if (!side(n) || !stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!workspace) return SPINNER_ERR_WORKSPACE;
+    if (!aligned16(w_codes) || !aligned16(out) || !aligned16(workspace)) return SPINNER_ERR_ALIGNMENT;
+    uint8_t* codes = static_cast<uint8_t*>(workspace);
+    uint8_t* scales = codes + (size_t)rows * (k / 2);
+    rc = spinner_mx_quantize(x, dtype, rows, k, x_stride, diag, block, codes, scales, stream);
+    if (rc != SPINNER_OK) return rc;
+    return spinner_mx_matmul(codes, scales, rows, k, w_codes, w_scales, n, experts, ends, out, dtype, out_stride, stream);
+}
+
+// forward and dx: rows of `depth` numbers against w [experts][n][k]
+static int grouped(int direction, const void* a, int dtype, long rows, long a_stride, const void* w, int n, int k, int experts,
+                   const long long* ends, void* out, long out_stride, void* stream)
+{
+    if (!type16(dtype)) return SPINNER_ERR_BAD_TYPE;
+    const int rc = check_groups(rows, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    const bool forward = direction == spinner::kForward;
+    if (!side(n) || !side(k) || !stride_in(a_stride) || !stride_out(out_stride, forward ? n : k, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!a || !w || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(a) || !aligned16(w) || !aligned16(out)) return SPINNER_ERR_ALIGNMENT;
+    spinner::ProductParams p = {};
+    p.a = static_cast<const char*>(a);
+    p.b = static_cast<const char*>(w);
+    p.out = static_cast<char*>(out);
+    p.ends = ends;
+    p.a_stride = 2LL * a_stride;
+    p.b_stride = 2LL * k;
+    p.b_group = 2LL * n * k;
+    p.out_stride = out_stride;
+    p.rows = (int)rows;
+    p.experts = experts;
+    p.width = forward ? n : k;
+    p.depth = forward ? k : n;
+    const auto launch = dtype == SPINNER_BF16 ? spinner::launch_product_bf16 : spinner::launch_product_f16;
+    return launched(launch(direction, dtype, p, static_cast<hipStream_t>(stream)));
+}
+
+int spinner_grouped_matmul(const void* x, int dtype, long rows, int k, long x_stride, const void* w, int n, int experts,
+                           const long long* ends, void* out, long out_stride, void* stream)
+{
+    return grouped(spinner::kForward, x, dtype, rows, x_stride, w, n, k, experts, ends, out, out_stride, stream);
+}
+
+int spinner_grouped_matmul_dx(const void* dy, int dtype, long rows, int n, long dy_stride, const void* w, int k, int experts,
+                              const long long* ends, void* dx, long dx_stride, void* stream)
+{
+    return grouped(spinner::kDx, dy, dtype, rows, dy_stride, w, n, k, experts, ends, dx, dx_stride, stream);
+}
+
+int spinner_grouped_matmul_dw(const void* dy, const void* x, int dtype, long rows, int n, int k, long dy_stride, long x_stride,
+                              int experts, const long long* ends, void* dw, int dw_dtype, void* stream)
+{
+    if (!type16(dtype) || (dw_dtype != dtype && dw_dtype != SPINNER_F32)) return SPINNER_ERR_BAD_TYPE;
+    const int rc = check_groups(rows, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    if (!side(n) || !side(k) || !stride_in(dy_stride) || !stride_in(x_stride)) return SPINNER_ERR_BAD_SHAPE;
+    if ((rows && (!dy || !x)) || !dw) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(dw)) return SPINNER_ERR_ALIGNMENT;
+    spinner::ProductParams p = {};
+    p.a = static_cast<const char*>(dy);
+    p.b = static_cast<const char*>(x);
+    p.out = static_cast<char*>(dw);
+    p.ends = ends;
+    p.a_stride = 2LL * dy_stride;
+    p.b_stride = 2LL * x_stride;
+    p.out_stride = k;
+    p.rows = (int)rows;
+    p.experts = experts;
+    p.height = n;
+    p.width = k;
+    const auto launch = dtype == SPINNER_BF16 ? spinner::launch_product_bf16 : spinner::launch_product_f16;
+    return launched(launch(spinner::kDw, dw_dtype, p, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

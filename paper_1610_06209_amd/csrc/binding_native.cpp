@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
 #include <pybind11/pybind11.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -456,10 +457,242 @@ ENTRY(struct_apply_ws, 10)
     return THPVariable_Wrap(std::move(out));
 ENTRY_END
 
+// ---- 4-bit numbers and products of rows grouped by expert
+bool element_type(at::ScalarType t, int* code)
+{
+    if (t == at::kFloat) *code = SPINNER_F32;
+    else if (t == at::kBFloat16) *code = SPINNER_BF16;
+    else if (t == at::kHalf) *code = SPINNER_F16;
+    else return false;
+    return true;
+}
+bool dtype_of(PyObject* o, at::ScalarType* type, int* code)
+{
+    if (!THPDtype_Check(o)) return false;
+    *type = reinterpret_cast<THPDtype*>(o)->scalar_type;
+    return element_type(*type, code);
+}
+// contiguous rows of plain numbers on the GPU that the call runs on
+const Tensor* number_rows(PyObject* o, long* count, int* width, int* code)
+{
+    const Tensor* t = gpu_tensor(o);
+    if (!t || t->dim() != 2 || t->size(1) > INT_MAX || !element_type(t->scalar_type(), code)) return nullptr;
+    if (t->get_device() != c10::hip::current_device()) return nullptr;
+    *count = (long)t->size(0);
+    *width = (int)t->size(1);
+    return t;
+}
+const Tensor* byte_rows(PyObject* o, long count, int64_t width)
+{
+    const Tensor* t = typed_tensor(o, at::kByte);
+    return t && t->dim() == 2 && t->size(0) == count && t->size(1) == width ? t : nullptr;
+}
+// [n][k] or [experts][n][k]
+bool weights(const Tensor* t, int* experts, int* n, int64_t* k)
+{
+    if (!t || (t->dim() != 2 && t->dim() != 3) || t->size(-2) > INT_MAX || t->size(0) > INT_MAX) return false;
+    *experts = t->dim() == 3 ? (int)t->size(0) : 1;
+    *n = (int)t->size(-2);
+    *k = t->size(-1);
+    return true;
+}
+bool expert_ends(PyObject* o, int experts, const long long** ends)
+{
+    *ends = nullptr;
+    if (o == Py_None) return experts == 1;
+    const Tensor* t = typed_tensor(o, at::kLong);
+    if (!t || t->dim() != 1 || t->numel() != experts) return false;
+    *ends = static_cast<const long long*>(t->data_ptr());
+    return true;
+}
+bool result_rows(PyObject* o, const Tensor** given, at::ScalarType type, long count, int width)
+{
+    *given = nullptr;
+    if (o == Py_None) return true;
+    const Tensor* t = typed_tensor(o, type);
+    if (!t || t->dim() != 2 || t->size(0) != count || t->size(1) != width) return false;
+    *given = t;
+    return true;
+}
+Tensor result(const Tensor* given, at::IntArrayRef sizes, at::ScalarType type, const Tensor& like)
+{
+    return given ? *given : at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
+}
+bool rotation(PyObject* diag, PyObject* block, int k, const Tensor** d, int* b)
+{
+    *d = nullptr;
+    if (!whole(block, b)) return false;
+    if (diag == Py_None) return true;
+    *d = floats(diag, k);
+    return *d && (*d)->dim() == 1;
+}
+
+// x, diag, block, codes, scales, stream
+ENTRY(mx_quantize, 6)
+    long count;
+    int k, code, block;
+    const Tensor *x = number_rows(a[0], &count, &k, &code), *d, *gc = nullptr, *gs = nullptr;
+    if (!x || a[5] != Py_None || k % 32 || !rotation(a[1], a[2], k, &d, &block)) LONG_WAY;
+    if (a[3] != Py_None && !(gc = byte_rows(a[3], count, k / 2))) LONG_WAY;
+    if (a[4] != Py_None && !(gs = byte_rows(a[4], count, k / 32))) LONG_WAY;
+    Tensor codes, scales;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        codes = result(gc, {count, k / 2}, at::kByte, *x);
+        scales = result(gs, {count, k / 32}, at::kByte, *x);
+        rc = spinner_mx_quantize(ptr<void>(x), code, count, k, k, ptr(d), block, ptr<void>(codes), ptr<void>(scales), current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    PyObject *c = THPVariable_Wrap(std::move(codes)), *s = c ? THPVariable_Wrap(std::move(scales)) : nullptr;
+    if (!s) { Py_XDECREF(c); return nullptr; }
+    PyObject* both = PyTuple_Pack(2, c, s);
+    Py_DECREF(c);
+    Py_DECREF(s);
+    return both;
+ENTRY_END
+
+// codes, scales, dtype, out, stream
+ENTRY(mx_dequantize, 5)
+    const Tensor *codes = typed_tensor(a[0], at::kByte), *given;
+    at::ScalarType type;
+    int code;
+    if (!codes || codes->dim() != 2 || codes->size(1) % 16 || codes->size(1) > INT_MAX / 2 || a[4] != Py_None || !dtype_of(a[2], &type, &code)) LONG_WAY;
+    if (codes->get_device() != c10::hip::current_device()) LONG_WAY;
+    const long count = (long)codes->size(0);
+    const int k = 2 * (int)codes->size(1);
+    const Tensor* scales = byte_rows(a[1], count, k / 32);
+    if (!scales || !result_rows(a[3], &given, type, count, k)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, k}, type, *codes);
+        rc = spinner_mx_dequantize(ptr<void>(codes), ptr<void>(scales), count, k, ptr<void>(out), code, k, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream
+ENTRY(mx_matmul, 8)
+    const Tensor *codes = typed_tensor(a[0], at::kByte), *wc = typed_tensor(a[2], at::kByte), *ws = typed_tensor(a[3], at::kByte), *given;
+    at::ScalarType type;
+    int code, experts, n, experts_s, n_s;
+    int64_t half, blocks;
+    const long long* ends;
+    if (!codes || codes->dim() != 2 || codes->size(1) % 16 || codes->size(1) > INT_MAX / 2 || a[7] != Py_None || !dtype_of(a[5], &type, &code)) LONG_WAY;
+    if (codes->get_device() != c10::hip::current_device()) LONG_WAY;
+    const long count = (long)codes->size(0);
+    const int k = 2 * (int)codes->size(1);
+    const Tensor* scales = byte_rows(a[1], count, k / 32);
+    if (!scales || !weights(wc, &experts, &n, &half) || !weights(ws, &experts_s, &n_s, &blocks) || half != k / 2 || blocks != k / 32) LONG_WAY;
+    if (wc->dim() != ws->dim() || experts_s != experts || n_s != n || !expert_ends(a[4], experts, &ends) || !result_rows(a[6], &given, type, count, n)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, n}, type, *codes);
+        rc = spinner_mx_matmul(ptr<void>(codes), ptr<void>(scales), count, k, ptr<void>(wc), ptr<void>(ws), n, experts, ends, ptr<void>(out),
+                                code, n, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// x, w_codes, w_scales, diag, block, ends, out, workspace, stream
+ENTRY(mx_linear, 9)
+    long count;
+    int k, code, block, experts, n, experts_s, n_s;
+    int64_t half, blocks;
+    const long long* ends;
+    const Tensor *x = number_rows(a[0], &count, &k, &code), *wc = typed_tensor(a[1], at::kByte), *ws = typed_tensor(a[2], at::kByte), *d, *given;
+    if (!x || a[8] != Py_None || k % 32 || !rotation(a[3], a[4], k, &d, &block)) LONG_WAY;
+    if (!weights(wc, &experts, &n, &half) || !weights(ws, &experts_s, &n_s, &blocks) || half != k / 2 || blocks != k / 32) LONG_WAY;
+    if (wc->dim() != ws->dim() || experts_s != experts || n_s != n || !expert_ends(a[5], experts, &ends)) LONG_WAY;
+    if (!result_rows(a[6], &given, x->scalar_type(), count, n)) LONG_WAY;
+    const size_t need = spinner_mx_linear_workspace_bytes(count, k);
+    Buffer w;
+    if (!w.usable_bytes(a[7], need)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, n}, x->scalar_type(), *x);
+        const Tensor scratch = w.scratch(need, *x);
+        rc = spinner_mx_linear(ptr<void>(x), code, count, k, k, ptr(d), block, ptr<void>(wc), ptr<void>(ws), n, experts, ends, ptr<void>(out), n,
+                                ptr<void>(scratch), current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+PyObject* grouped(Args a, bool across)
+{
+    long count;
+    int depth, code, experts, n;
+    int64_t k;
+    const long long* ends;
+    const Tensor *x = number_rows(a[0], &count, &depth, &code), *w = gpu_tensor(a[1]), *given;
+    if (!x || a[4] != Py_None || !weights(w, &experts, &n, &k) || k > INT_MAX || w->scalar_type() != x->scalar_type()) LONG_WAY;
+    if (depth != (across ? k : n) || !expert_ends(a[2], experts, &ends)) LONG_WAY;
+    const int width = across ? n : (int)k;
+    if (!result_rows(a[3], &given, x->scalar_type(), count, width)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, width}, x->scalar_type(), *x);
+        rc = (across ? spinner_grouped_matmul : spinner_grouped_matmul_dx)(ptr<void>(x), code, count, depth, depth, ptr<void>(w), width, experts, ends,
+                                                                           ptr<void>(out), width, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+}
+// x, w, ends, out, stream
+ENTRY(grouped_matmul, 5)
+    return grouped(a, true);
+ENTRY_END
+// dy, w, ends, dx, stream
+ENTRY(grouped_matmul_dx, 5)
+    return grouped(a, false);
+ENTRY_END
+
+// dy, x, ends, dtype, dw, stream
+ENTRY(grouped_matmul_dw, 6)
+    long count, x_count;
+    int n, k, code, x_code, dw_code, experts = 1;
+    at::ScalarType type;
+    const long long* ends = nullptr;
+    const Tensor *dy = number_rows(a[0], &count, &n, &code), *x = number_rows(a[1], &x_count, &k, &x_code), *given = nullptr;
+    if (!dy || !x || a[5] != Py_None || x_count != count || x_code != code || !dtype_of(a[3], &type, &dw_code)) LONG_WAY;
+    if (a[2] != Py_None) {
+        const Tensor* e = typed_tensor(a[2], at::kLong);
+        if (!e || e->dim() != 1 || e->numel() < 1 || e->numel() > INT_MAX) LONG_WAY;
+        experts = (int)e->numel();
+        ends = static_cast<const long long*>(e->data_ptr());
+    }
+    const std::vector<int64_t> sizes = ends ? std::vector<int64_t>{experts, n, k} : std::vector<int64_t>{n, k};
+    if (a[4] != Py_None) {
+        given = typed_tensor(a[4], type);
+        if (!given || given->sizes() != at::IntArrayRef(sizes)) LONG_WAY;
+    }
+    Tensor dw;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        dw = result(given, sizes, type, *dy);
+        rc = spinner_grouped_matmul_dw(ptr<void>(dy), ptr<void>(x), code, count, n, k, n, k, experts, ends, ptr<void>(dw), dw_code, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(dw));
+ENTRY_END
+
 #define METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(apply_signs), METHOD(apply), METHOD(apply_blocks), METHOD(hash), METHOD(hash_signs), METHOD(sign_codes),
                          METHOD(sign_codes_signs), METHOD(angular_gram), METHOD(layer_forward), METHOD(layer_backward), METHOD(sketch),
-                         METHOD(sketch_gram), METHOD(struct_apply_ws), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(sketch_gram), METHOD(struct_apply_ws), METHOD(mx_quantize), METHOD(mx_dequantize), METHOD(mx_matmul),
+                         METHOD(mx_linear), METHOD(grouped_matmul), METHOD(grouped_matmul_dx), METHOD(grouped_matmul_dw), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

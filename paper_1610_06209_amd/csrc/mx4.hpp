@@ -1,0 +1,52 @@
+// Microscaled 4-bit floating point and grouped matrix products: what the host code and the kernels share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace spinner {
+
+// element types, in the order of spinner_dtype_t; kMx4 is internal (4-bit operands)
+enum { kF32 = 0, kBf16 = 1, kF16 = 2, kMx4 = 3 };
+
+constexpr int kMx4Block = 32;             // numbers that share a scale
+constexpr int kMaxRotation = 4096;        // longest run of coordinates that one rotation mixes
+constexpr int kMaxExperts = 1024;
+
+struct QuantizeParams {
+    const void* x;
+    const float* diag;                    // null: all ones
+    uint8_t* codes;
+    uint8_t* scales;
+    long long x_stride;                   // elements
+    int rows, k;
+};
+// block: 0 (no rotation) or a power of two in [32, kMaxRotation]
+hipError_t launch_mx4_quantize(const QuantizeParams& p, int dtype, int block, hipStream_t s);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int rows, int k, void* out, int dtype,
+                                 long long out_stride, hipStream_t s);
+
+// The three products of a layer with weights w[expert][n][k] on rows that are grouped by expert (group e: rows
+// [ends[e - 1], ends[e]); without ends all rows are one group):
+enum { kForward = 0,      // out[row][n] = sum_k a[row][k] b[e][n][k]
+       kDx = 1,           // out[row][k] = sum_n a[row][n] b[e][n][k]
+       kDw = 2 };         // out[e][n][k] = sum_row a[row][n] b[row][k]
+struct ProductParams {
+    const char* a;                        // operand of the result's rows
+    const char* b;                        // operand of the result's columns
+    const uint8_t* a_scales;              // kMx4
+    const uint8_t* b_scales;
+    char* out;
+    const long long* ends;                // null: one group
+    long long a_stride, b_stride;         // bytes from one row of the operand, as it lies, to the next
+    long long b_group;                    // kForward, kDx: bytes from one expert's weights to the next
+    long long out_stride;                 // elements from one row of the result to the next
+    int rows, experts;
+    int height;                           // kDw: rows of one expert's result
+    int width;                            // columns of the result
+    int depth;                            // kForward, kDx: numbers in a sum
+};
+hipError_t launch_product_mx4(int out_type, const ProductParams& p, hipStream_t s);           // kForward
+hipError_t launch_product_bf16(int direction, int out_type, const ProductParams& p, hipStream_t s);
+hipError_t launch_product_f16(int direction, int out_type, const ProductParams& p, hipStream_t s);
+
+}  // namespace spinner

@@ -1,0 +1,15 @@
+// Products of 4-bit operands (see product_kernels.hpp).
+#include "product_kernels.hpp"
+
+namespace spinner {
+
+hipError_t launch_product_mx4(int out_type, const ProductParams& p, hipStream_t s)
+{
+    switch (out_type) {
+    case kF32: return launch_product_as<kForward, kMx4, float>(p, s);
+    case kBf16: return launch_product_as<kForward, kMx4, __bf16>(p, s);
+    default: return launch_product_as<kForward, kMx4, _Float16>(p, s);
+    }
+}
+
+}  // namespace spinner
