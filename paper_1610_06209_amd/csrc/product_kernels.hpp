@@ -11,15 +11,13 @@
 namespace spinner {
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// what lies beyond an operand's end reads as this
-__device__ const uintx4 zero_piece = {0, 0, 0, 0};
 
 // ------------------------------------------------------------------ groups of rows
 // inclusive sum / maximum over the lanes up to each one, of numbers >= 0
@@ -180,65 +178,70 @@ constexpr int kChunkBytes = 128;                          // of a row's depth in
 constexpr int kChunkPieces = kChunkBytes / 16;
 constexpr int kChunkDepth16 = kChunkBytes / 2;            // the same in 16-bit numbers
 constexpr int kChunkScales = kChunkBytes / 16;            // scales of a row's chunk: 32 numbers are 16 bytes
+constexpr unsigned kFar = 0x80000000u;                    // offsets of a tile's pieces stay below this
+
+// 16 bytes a lane from a buffer of kFar bytes at `from`, to 1 KiB of LDS.  Written out because the compiler, which counts these
+// loads like any others, would wait for all of them before each transposing read of LDS, whose place it does not follow; they
+// have no register to arrive in, and the kernel waits for them itself before the waves meet.
+__device__ __forceinline__ void load_to_lds(uintx4* to, const char* from, unsigned offset)
+{
+    const unsigned long long base = reinterpret_cast<unsigned long long>(from);
+    const intx4 buffer = {(int)base, (int)(base >> 32) & 0xffff, (int)kFar, 0x00027000};
+    const unsigned place = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)to);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(buffer), "s"(place) : "memory");
+}
 
 // An operand's part of a tile in LDS, SPAN rows (or columns) by a chunk of depth, and its way there.
-//   deep rows:  depth lies along the rows in memory.  LDS row r of 128 bytes, its piece p at p xor (r mod 8).
+//   deep rows:  depth lies along the rows in memory.  LDS row r of 128 bytes, its piece p at p xor (r / 2 mod 8): the sixteen lanes of a
+//               phase of a read, sixteen rows, then cover all banks.
 //   flat rows:  depth runs across the rows in memory (16-bit types).  LDS row d (of 64) of SPAN numbers; runs of 64 bytes lie exchanged
 //               by d, so that the four rows that a transposing read takes at once lie in different banks.
-template <bool DEEP, int SPAN, int WAVES>
+template <bool DEEP, int SPAN, int WAVES, bool ANY>
 struct TileOperand {
     static constexpr int kLoads = SPAN * kChunkBytes / 1024 / WAVES;      // of 16 bytes a lane, per wave and chunk
     static constexpr int kRowPieces = DEEP ? kChunkPieces : SPAN / 8;
     static constexpr int kRowsALoad = 64 / kRowPieces;
     static_assert(kLoads >= 1, "a wave loads something");
+    using Offset = std::conditional_t<ANY, long long, unsigned>;          // from the tile's first number; what is not ANY lies within kFar
 
     static __device__ __forceinline__ int exchanged(int d) { return SPAN * 2 >= 256 ? d & 3 : (d >> 1) & 1; }
-
-    const char* from[kLoads];      // this lane's pieces of the first chunk
-    int need[kLoads];              // deep: byte of depth where the piece starts; flat: depth of the row, or past every end where the column is
-    int numbers[kLoads];           // flat, and pieces that may be cut: numbers of the piece inside the row
-
-    // base: first row and column of the tile; rows_left: rows (deep) / columns (flat) of the operand from there on
-    __device__ __forceinline__ void start(const char* base, long long stride, int left, int wave, int lane)
+    // row in LDS and piece of it in memory of this lane's t-th load
+    static __device__ __forceinline__ int load_row(int t, int wave, int lane) { return (wave * kLoads + t) * kRowsALoad + lane / kRowPieces; }
+    static __device__ __forceinline__ int load_piece(int r, int lane)
     {
+        return (lane % kRowPieces) ^ (DEEP ? (r >> 1) & 7 : exchanged(r) << 2);
+    }
+
+    Offset offset[kLoads];
+    int left;                      // rows (deep) / columns (flat) of the operand from the tile's first on
+
+    __device__ __forceinline__ void start(long long stride, int left_, int wave, int lane)
+    {
+        left = left_;
 #pragma unroll
         for (int t = 0; t < kLoads; ++t) {
-            const int r = (wave * kLoads + t) * kRowsALoad + lane / kRowPieces, q = lane % kRowPieces;
-            if constexpr (DEEP) {
-                const int piece = q ^ (r & 7), row = r < left ? r : left - 1;
-                from[t] = base + row * stride + piece * 16;
-                need[t] = piece * 16;
-            } else {
-                const int piece = q ^ (exchanged(r) << 2);
-                from[t] = base + r * stride + piece * 16;
-                need[t] = r;
-                numbers[t] = left - piece * 8;
-            }
+            const int r = load_row(t, wave, lane), row = DEEP && r >= left ? left - 1 : r;
+            offset[t] = (Offset)row * (Offset)stride + load_piece(r, lane) * 16;
+            if (!DEEP && !ANY && load_piece(r, lane) * 8 >= left) offset[t] = kFar;
         }
     }
-    // straight to LDS; depth_left: bytes (deep) / rows (flat) of depth from this chunk on
-    template <bool WHOLE>
-    __device__ __forceinline__ void load(uintx4* lds, long long advance, int depth_left, int wave) const
+    // Load T of those of the chunk that starts at `from`, straight to LDS; depth_left: bytes (deep) / rows (flat) of depth from there on.
+    // What lies beyond the operand is asked for beyond the end of the buffer as the load knows it, and arrives as zeros.
+    template <int T>
+    __device__ __forceinline__ void load(uintx4* lds, const char* from, int depth_left, int wave, int lane) const
     {
-#pragma unroll
-        for (int t = 0; t < kLoads; ++t) {
-            const char* p = from[t] + advance;
-            if (!WHOLE && need[t] >= depth_left) p = reinterpret_cast<const char*>(&zero_piece);
-            if constexpr (!DEEP)
-                if (numbers[t] <= 0) p = reinterpret_cast<const char*>(&zero_piece);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                             (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + t) * 64), 16, 0, 0);
-        }
+        const int r = load_row(T, wave, lane);
+        const bool there = DEEP ? load_piece(r, lane) * 16 < depth_left : r < depth_left;
+        load_to_lds(lds + (wave * kLoads + T) * 64, from, there ? (unsigned)offset[T] : kFar);
     }
     // through registers, from any alignment
-    __device__ __forceinline__ void fetch(uintx4 (&v)[kLoads], long long advance, int depth_left) const
+    __device__ __forceinline__ void fetch(uintx4 (&v)[kLoads], const char* from, int depth_left, int wave, int lane) const
     {
 #pragma unroll
         for (int t = 0; t < kLoads; ++t) {
-            int count;
-            if constexpr (DEEP) count = (depth_left - need[t]) >> 1;
-            else count = need[t] < depth_left ? numbers[t] : 0;
-            v[t] = fetch_some(from[t] + advance, count);
+            const int r = load_row(t, wave, lane), piece = load_piece(r, lane);
+            const int count = DEEP ? (depth_left - piece * 16) >> 1 : (r < depth_left ? left - piece * 8 : 0);
+            v[t] = fetch_some(from + offset[t], count);
         }
     }
     __device__ __forceinline__ void put(const uintx4 (&v)[kLoads], uintx4* lds, int wave, int lane) const
@@ -252,7 +255,7 @@ struct TileOperand {
         const int g = lane >> 5;
         if constexpr (DEEP) {
             const int r = first + (lane & 31);
-            return lds[r * kChunkPieces + ((2 * s + g) ^ (r & 7))];
+            return lds[r * kChunkPieces + ((2 * s + g) ^ ((r >> 1) & 7))];
         } else {
             // lane groups of 16: four rows of depth by 16 columns each read, which arrive as one column a lane
             const int j = lane & 15, col = first + ((lane >> 4) & 1) * 16 + (j & 3) * 4;
@@ -269,27 +272,35 @@ struct TileOperand {
     }
 };
 
-// The scales of a chunk for a lane's row of each 32: eight bytes, shifted so that a lane's own of each step's two is byte 0 or 2.
-struct ChunkScales {
-    unsigned w[2];
-    __device__ __forceinline__ void fetch(const uint8_t* p, int left)
+// Scales of a tile's rows go through LDS, two chunks' (16 bytes of a row) at a time: straight from memory, eight bytes a row and chunk, they
+// made twice as many requests as the numbers themselves.
+struct RowScales {
+    unsigned w[4];
+    int beyond;                    // bytes that the operand's end lies in front of the last byte asked for
+    // at: place of the first scale wanted, from the tile's first on; end: place behind the operand's last one; before: sixteen bytes in front of the
+    // tile's first.  What the end cuts is read as the sixteen bytes in front of the end.
+    __device__ __forceinline__ void fetch(const uint8_t* before, unsigned at, unsigned end)
     {
-        if (left >= kChunkScales) {
-            struct __attribute__((packed, aligned(1))) Eight { unsigned w[2]; };
-            const Eight t = *reinterpret_cast<const Eight*>(p);
-            w[0] = t.w[0];
-            w[1] = t.w[1];
-        } else {
-            w[0] = w[1] = 0x7f7f7f7fu;             // ones: the numbers there are zeros
+        const unsigned from = at + 16 < end ? at + 16 : end;
+        struct __attribute__((packed, aligned(1))) Sixteen { unsigned w[4]; };
+        const Sixteen t = *reinterpret_cast<const Sixteen*>(before + from);
 #pragma unroll
-            for (int i = 0; i < kChunkScales - 1; ++i)
-                if (i < left) w[i >> 2] = (w[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (unsigned)p[i] << (8 * (i & 3));
-        }
+        for (int i = 0; i < 4; ++i) w[i] = t.w[i];
+        beyond = (int)(at + 16 - from);
     }
-    __device__ __forceinline__ void own(int lane)
+    // behind the row's last scale (`left` are its own) come ones: the numbers there are zeros, but a NaN would stay one
+    __device__ __forceinline__ void put(uintx4* to, int left) const
     {
-        w[0] >>= (lane >> 5) * 8;
-        w[1] >>= (lane >> 5) * 8;
+        unsigned long long lo = w[0] | (unsigned long long)w[1] << 32, hi = w[2] | (unsigned long long)w[3] << 32;
+        const int s = 8 * (beyond & 7);
+        if (beyond & 8) { lo = hi; hi = 0; }
+        lo = lo >> s | (s ? hi << (64 - s) : 0);
+        hi >>= s;
+        const unsigned long long ml = left >= 8 ? ~0ull : (left > 0 ? (1ull << (8 * left)) - 1 : 0);
+        const unsigned long long mh = left >= 16 ? ~0ull : (left > 8 ? (1ull << (8 * (left - 8))) - 1 : 0);
+        lo = (lo & ml) | (0x7f7f7f7f7f7f7f7full & ~ml);
+        hi = (hi & mh) | (0x7f7f7f7f7f7f7f7full & ~mh);
+        *to = uintx4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
     }
 };
 
@@ -299,11 +310,10 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
 {
     constexpr int WAVES = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr bool MX = TYPE == kMx4;
-    using A = TileOperand<DIRECTION != kDw, BM, WAVES>;
-    using B = TileOperand<DIRECTION == kForward, BN, WAVES>;
-    // two buffers, each read and written in code of its own, so that the compiler sees that what is read is not what the loads in
-    // flight write
+    using A = TileOperand<DIRECTION != kDw, BM, WAVES, ANY>;
+    using B = TileOperand<DIRECTION == kForward, BN, WAVES, ANY>;
     __shared__ uintx4 even[(BM + BN) * kChunkPieces], odd[(BM + BN) * kChunkPieces];
+    __shared__ uintx4 row_scales[MX ? 2 : 1][MX ? BM + BN : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const unsigned columns = (unsigned)(p.width + BN - 1) / BN;
@@ -313,6 +323,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
     int rows_left, cols_left, depth;          // depth: bytes (kForward, kDx: of A's rows), rows (kDw)
     Out* out = reinterpret_cast<Out*>(p.out);
     const uint8_t *a_scales = nullptr, *b_scales = nullptr;
+    unsigned a_end = 0, b_end = 0;            // scales from the tile's first to the operand's last
     if constexpr (DIRECTION == kDw) {
         // an equal share of every expert's tiles to each XCD: the depth of an expert's sums is the number of its rows
         const unsigned per_expert = columns * ((unsigned)(p.height + BM - 1) / BM), share = (per_expert + 7) / 8;
@@ -355,17 +366,21 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
         depth = nobody ? 0 : (MX ? p.depth / 2 : p.depth * 2);
         out += at.lo * p.out_stride + n0;
         if constexpr (MX) {
-            const long long row_scales = p.depth / kMx4Block;
-            a_scales = p.a_scales + at.lo * row_scales;
-            b_scales = p.b_scales + ((nobody ? 0 : at.expert) * (long long)p.width + n0) * row_scales;
+            const long long count = p.depth / kMx4Block;
+            const long long from_a = at.lo * count, from_b = ((nobody ? 0 : at.expert) * (long long)p.width + n0) * count;
+            const long long a_left = p.rows * count - from_a, b_left = p.experts * (p.width * count) - from_b;
+            a_scales = p.a_scales + from_a - 16;
+            b_scales = p.b_scales + from_b - 16;
+            a_end = (unsigned)(a_left < kFar ? a_left : kFar);
+            b_end = (unsigned)(b_left < kFar ? b_left : kFar);
         }
     }
     const int m_rows = rows_left < BM ? rows_left : BM;
 
     A oa;
     B ob;
-    oa.start(a, p.a_stride, rows_left, wave, lane);
-    ob.start(b, p.b_stride, cols_left, wave, lane);
+    oa.start(p.a_stride, rows_left, wave, lane);
+    ob.start(p.b_stride, cols_left, wave, lane);
     floatx16 acc[TM][TN];
 #pragma unroll
     for (int t = 0; t < TM; ++t)
@@ -375,92 +390,146 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
             for (int v = 0; v < 16; ++v) acc[t][u][v] = 0.0f;
 
     // depth in units of an operand: bytes along deep rows, rows of flat ones
-    const int chunks = DIRECTION == kDw ? (depth + kChunkDepth16 - 1) / kChunkDepth16 : (depth + kChunkBytes - 1) / kChunkBytes;
-    const auto left_a = [&](int c) { return DIRECTION == kDw ? depth - c * kChunkDepth16 : depth - c * kChunkBytes; };
-    const auto left_b = [&](int c) { return DIRECTION == kDx ? depth / 2 - c * kChunkDepth16 : left_a(c); };
+    constexpr int unit_a = DIRECTION == kDw ? kChunkDepth16 : kChunkBytes, unit_b = DIRECTION == kForward ? kChunkBytes : kChunkDepth16;
+    const int depth_b = DIRECTION == kDx ? depth / 2 : depth;
+    const int chunks = (depth + unit_a - 1) / unit_a;
     const long long step_a = DIRECTION == kDw ? kChunkDepth16 * p.a_stride : kChunkBytes;
     const long long step_b = DIRECTION == kForward ? kChunkBytes : kChunkDepth16 * p.b_stride;
 
     uintx4 va[ANY ? A::kLoads : 1], vb[ANY ? B::kLoads : 1];
-    const auto load = [&](int c, uintx4* buffer) {
-        const bool whole = DIRECTION == kDw ? left_a(c) >= kChunkDepth16 : left_a(c) >= kChunkBytes;
+    const auto fetch = [&](int c) {
         if constexpr (ANY) {
-            oa.fetch(va, c * step_a, left_a(c));
-            ob.fetch(vb, c * step_b, left_b(c));
-        } else if (whole) {
-            oa.template load<true>(buffer, c * step_a, 0, wave);
-            ob.template load<true>(buffer + BM * kChunkPieces, c * step_b, 0, wave);
-        } else {
-            oa.template load<false>(buffer, c * step_a, left_a(c), wave);
-            ob.template load<false>(buffer + BM * kChunkPieces, c * step_b, left_b(c), wave);
+            oa.fetch(va, a + c * step_a, depth - c * unit_a, wave, lane);
+            ob.fetch(vb, b + c * step_b, depth_b - c * unit_b, wave, lane);
         }
     };
-    ChunkScales sa[MX ? TM : 1], sb[MX ? TN : 1];
-    const uint8_t *from_sa[MX ? TM : 1], *from_sb[MX ? TN : 1];
-    const auto load_scales = [&](int c) {
-        if constexpr (MX) {
-            const int left = p.depth / kMx4Block - c * kChunkScales;
-#pragma unroll
-            for (int t = 0; t < TM; ++t) sa[t].fetch(from_sa[t] + c * kChunkScales, left);
-#pragma unroll
-            for (int u = 0; u < TN; ++u) sb[u].fetch(from_sb[u] + c * kChunkScales, left);
+    const auto put = [&](uintx4* buffer) {
+        if constexpr (ANY) {
+            oa.put(va, buffer, wave, lane);
+            ob.put(vb, buffer + BM * kChunkPieces, wave, lane);
         }
     };
-    if constexpr (MX) {
-        const long long row_scales = p.depth / kMx4Block;
+    // Scales (kMx4): every thread brings those of some rows for a pair of chunks; a lane takes the eight bytes of its rows for one chunk, shifted
+    // so that its own of each step's two is byte 0 or 2.
+    constexpr int THREADS = 64 * WAVES, kScaleRows = MX ? (BM + BN) / THREADS : 1;
+    static_assert(!MX || (BM % THREADS == 0 || THREADS % BM == 0) && (BM + BN) % THREADS == 0, "whole rows a thread");
+    const int scale_count = MX ? p.depth / kMx4Block : 0;
+    RowScales brought[kScaleRows];
+    const auto fetch_scales = [&](int c) {
 #pragma unroll
-        for (int t = 0; t < TM; ++t) {
-            const int r = (wm * TM + t) * 32 + (lane & 31);
-            from_sa[t] = a_scales + (r < rows_left ? r : rows_left - 1) * row_scales;
+        for (int i = 0; i < kScaleRows; ++i) {
+            const int r = i * THREADS + (int)threadIdx.x;
+            const int ra = r < rows_left ? r : rows_left - 1, rb = r - BM < cols_left ? r - BM : cols_left - 1;
+            const unsigned at = (unsigned)((r < BM ? ra : rb) * scale_count + c * kChunkScales);
+            brought[i].fetch(r < BM ? a_scales : b_scales, at, r < BM ? a_end : b_end);
         }
+    };
+    const auto put_scales = [&](int c) {
 #pragma unroll
-        for (int u = 0; u < TN; ++u) {
-            const int r = (wn * TN + u) * 32 + (lane & 31);
-            from_sb[u] = b_scales + (r < cols_left ? r : cols_left - 1) * row_scales;
-        }
-    }
-    const auto chunk = [&](int c, const uintx4* now, uintx4* next) {
-        if constexpr (ANY) {
-            oa.put(va, const_cast<uintx4*>(now), wave, lane);
-            ob.put(vb, const_cast<uintx4*>(now) + BM * kChunkPieces, wave, lane);
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wave's pieces are in place
-        }
-        __syncthreads();                                          // everyone's are, and the other buffer has been read
-        ChunkScales ta[MX ? TM : 1], tb[MX ? TN : 1];
-        if constexpr (MX) {
+        for (int i = 0; i < kScaleRows; ++i) brought[i].put(&row_scales[c >> 1 & 1][i * THREADS + threadIdx.x], scale_count - c * kChunkScales);
+    };
+    uint2 sa[MX ? TM : 1], sb[MX ? TN : 1];
+    const auto take_scales = [&](int c) {
+        const char* from = reinterpret_cast<const char*>(&row_scales[c >> 1 & 1][lane & 31]) + (c & 1) * kChunkScales;
 #pragma unroll
-            for (int t = 0; t < TM; ++t) { ta[t] = sa[t]; ta[t].own(lane); }
+        for (int t = 0; t < TM; ++t) sa[t] = *reinterpret_cast<const uint2*>(from + (wm * TM + t) * 32 * 16);
 #pragma unroll
-            for (int u = 0; u < TN; ++u) { tb[u] = sb[u]; tb[u].own(lane); }
-        }
-        if (c + 1 < chunks) {
-            load(c + 1, next);
-            load_scales(c + 1);
-        }
-        static_for<0, 4>([&](auto s) {
-            uintx4 fa[TM], fb[TN];
+        for (int u = 0; u < TN; ++u) sb[u] = *reinterpret_cast<const uint2*>(from + (BM + (wn * TN + u) * 32) * 16);
+    };
+    uint2 ta[MX ? TM : 1], tb[MX ? TN : 1];
+    const auto own_scales = [&] {
+        const int shift = (lane >> 5) * 8;
 #pragma unroll
-            for (int t = 0; t < TM; ++t) fa[t] = A::operand(now, (wm * TM + t) * 32, s.value, lane);
+        for (int t = 0; t < TM; ++t) ta[t] = {sa[t].x >> shift, sa[t].y >> shift};
 #pragma unroll
-            for (int u = 0; u < TN; ++u) fb[u] = B::operand(now + BM * kChunkPieces, (wn * TN + u) * 32, s.value, lane);
-#pragma unroll
-            for (int t = 0; t < TM; ++t)
-#pragma unroll
-                for (int u = 0; u < TN; ++u) {
-                    // columns of the result along the instruction's rows: a lane then holds four neighbours of a row of `out`
-                    if constexpr (MX) acc[t][u] = multiply32_scaled<2 * (s.value & 1)>(fb[u], fa[t], acc[t][u], tb[u].w[s.value >> 1], ta[t].w[s.value >> 1]);
-                    else acc[t][u] = multiply32<TYPE>(fb[u], fa[t], acc[t][u]);
-                }
+        for (int u = 0; u < TN; ++u) tb[u] = {sb[u].x >> shift, sb[u].y >> shift};
+    };
+
+    uintx4 fa[2][TM], fb[2][TN];
+    // operand I of step S: the first rows' and all columns' come first, as they are multiplied
+    const auto operand = [&](const uintx4* buffer, auto s, auto i) {
+        constexpr int S = s.value, I = i.value;
+        if constexpr (I >= 1 && I <= TN) fb[S & 1][I - 1] = B::operand(buffer + BM * kChunkPieces, (wn * TN + I - 1) * 32, S, lane);
+        else fa[S & 1][I == 0 ? 0 : I - TN] = A::operand(buffer, (wm * TM + (I == 0 ? 0 : I - TN)) * 32, S, lane);
+    };
+    const auto operands = [&](const uintx4* buffer, auto s) { static_for<0, TM + TN>([&](auto i) { operand(buffer, s, i); }); };
+    // Step S: its products in turn with the reads of the next step's operands (step `next_s`, from `next`) and with loads of chunk `c` to
+    // LDS: of operand A (LOADS 1), of B (2).  The compiler keeps to this order.
+    const auto step = [&](auto s, const uintx4* next, auto next_s, auto loads, int c, uintx4* to) {
+        constexpr int S = s.value, LOADS = ANY ? 0 : loads.value, N = TM * TN, READS = TM + TN;
+        constexpr int COUNT = LOADS == 1 ? A::kLoads : (LOADS == 2 ? B::kLoads : 0);
+        static_for<0, N>([&](auto i) {
+            constexpr int I = i.value, t = I / TN, u = I % TN;
+            constexpr int rate = (READS + N - 1) / N;
+            static_for<I * rate, (I + 1) * rate < READS ? (I + 1) * rate : READS>([&](auto r) { operand(next, next_s, r); });
+            // columns of the result along the instruction's rows: a lane then holds four neighbours of a row of `out`
+            const uintx4 x = fa[S & 1][t], w = fb[S & 1][u];
+            if constexpr (MX) acc[t][u] = multiply32_scaled<2 * (S & 1)>(w, x, acc[t][u], S < 2 ? tb[u].x : tb[u].y, S < 2 ? ta[t].x : ta[t].y);
+            else acc[t][u] = multiply32<TYPE>(w, x, acc[t][u]);
+            static_for<I * COUNT / N, (I + 1) * COUNT / N>([&](auto l) {
+                if constexpr (LOADS == 1) oa.template load<l.value>(to, a + c * step_a, depth - c * unit_a, wave, lane);
+                else if constexpr (LOADS == 2) ob.template load<l.value>(to + BM * kChunkPieces, b + c * step_b, depth_b - c * unit_b, wave, lane);
+            });
+            __builtin_amdgcn_sched_barrier(0);
         });
     };
-    if (chunks > 0) {
-        load(0, even);
-        load_scales(0);
+    constexpr std::integral_constant<int, 0> s0{};
+    constexpr std::integral_constant<int, 1> s1{};
+    constexpr std::integral_constant<int, 2> s2{};
+    constexpr std::integral_constant<int, 3> s3{};
+    // every wave's pieces of the next chunk are in place, and the present one has been read
+    const auto meet = [&] {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    // A chunk is four steps, the operands of each read while the one before is multiplied.  Its last operands are read before the
+    // waves meet, so that its buffer is free for the chunk after the next from its last step on, and the first operands of the next
+    // chunk come during that step too.  FIRST: first of a pair, which brings the next pair's scales.
+    const auto chunk = [&](int c, uintx4* now, uintx4* next, auto first) {
+        if constexpr (MX) own_scales();
+        step(s0, now, s1, s2, c + 1, next);
+        if constexpr (MX && first.value) fetch_scales(c + 2);
+        step(s1, now, s2, s0, 0, nullptr);
+        step(s2, now, s3, s0, 0, nullptr);
+        put(next);
+        meet();
+        fetch(c + 2);
+        if constexpr (MX && first.value) put_scales(c + 2);
+        if constexpr (MX) take_scales(c + 1);
+        step(s3, next, s0, s1, c + 2, now);
+    };
+    // An odd number of chunks: the first by itself, out of the other buffer (4-bit operands: one of zeros behind the last).  Chunks behind the
+    // last are zeros, asked for and not multiplied.
+    const bool lone = !MX && (chunks & 1);
+    const auto begin = [&](uintx4* first, uintx4* second) {
+        if constexpr (ANY) {
+            fetch(0);
+            put(first);
+            fetch(1);
+        } else {
+            static_for<0, A::kLoads>([&](auto l) { oa.template load<l.value>(first, a, depth, wave, lane); });
+            static_for<0, B::kLoads>([&](auto l) { ob.template load<l.value>(first + BM * kChunkPieces, b, depth_b, wave, lane); });
+            static_for<0, A::kLoads>([&](auto l) { oa.template load<l.value>(second, a + step_a, depth - unit_a, wave, lane); });
+        }
+        if constexpr (MX) {
+            fetch_scales(0);
+            put_scales(0);
+        }
+        meet();
+        if constexpr (MX) take_scales(0);
+        operands(first, s0);
+    };
+    int c = 0;
+    if (lone) {
+        begin(odd, even);
+        chunk(0, odd, even, s0);
+        c = 1;
+    } else {
+        begin(even, odd);
     }
-    for (int c = 0; c < chunks; c += 2) {
-        chunk(c, even, odd);
-        if (c + 1 < chunks) chunk(c + 1, odd, even);
+    for (; c < chunks; c += 2) {
+        chunk(c, even, odd, s1);
+        chunk(c + 1, odd, even, s0);
     }
 
     // result register v of lane l: column 8 (v / 4) + 4 (l / 32) + v % 4, row l % 32 of its 32 x 32 tile
@@ -599,11 +668,13 @@ hipError_t launch_few_rows(const ProductParams& p, hipStream_t s)
     return hipGetLastError();
 }
 
-// whether every row that a kernel loads in pieces of 16 bytes is made of whole aligned ones
+// whether every row that a kernel loads in pieces of 16 bytes is made of whole aligned ones, and 256 rows lie within 32 bits
+constexpr long long kFarthestRow = 1 << 23;
 template <int DIRECTION, int TYPE>
 bool whole_pieces(const ProductParams& p)
 {
-    if (TYPE == kMx4) return true;                                    // rows of 16 bytes for each 32 numbers
+    if (TYPE == kMx4) return true;                                    // rows of 16 bytes for each 32 numbers, at most 2^23 bytes
+    if (p.a_stride > kFarthestRow || p.b_stride > kFarthestRow) return false;
     const int a_row = DIRECTION == kDw ? p.height : p.depth;
     const int b_row = DIRECTION == kForward ? p.depth : p.width;
     return a_row % 8 == 0 && b_row % 8 == 0 && p.a_stride % 16 == 0 && p.b_stride % 16 == 0 && p.b_group % 16 == 0;
@@ -614,12 +685,19 @@ hipError_t launch_product_as(const ProductParams& p, hipStream_t s)
 {
     if constexpr (DIRECTION == kForward) {
         const long long rows = (p.rows + p.experts - 1) / p.experts;      // of a group, on average
+        // (the tiles read scales sixteen at a time)
+        const long long scales = p.depth / kMx4Block;
+        if (TYPE == kMx4 && (p.rows * scales < 16 || p.experts * (p.width * scales) < 16)) return launch_few_rows<TYPE, 1, Out>(p, s);
         if (rows <= 16) return launch_few_rows<TYPE, 1, Out>(p, s);
         if (rows <= 32) return launch_few_rows<TYPE, 2, Out>(p, s);
         if (rows <= 64) return launch_few_rows<TYPE, 4, Out>(p, s);
     }
     if constexpr (TYPE != kMx4)
         if (!whole_pieces<DIRECTION, TYPE>(p)) return launch_tiles<DIRECTION, TYPE, 128, 128, 2, 2, true, Out>(p, s);
+    long long large;
+    if (DIRECTION == kDw) large = (long long)((p.height + 255) / 256) * ((p.width + 255) / 256) * p.experts;
+    else large = (long long)((p.rows + 255) / 256) * ((p.width + 255) / 256);
+    if (large >= 192) return launch_tiles<DIRECTION, TYPE, 256, 256, 2, 2, false, Out>(p, s);
     return launch_tiles<DIRECTION, TYPE, 128, 128, 2, 2, false, Out>(p, s);
 }
 
