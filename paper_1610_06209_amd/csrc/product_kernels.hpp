@@ -159,6 +159,23 @@ __device__ __forceinline__ void store_four(Out* p, float a, float b, float c, fl
     if (left > 3) p[3] = (Out)d;
 }
 
+// 16 bytes of neighbours of a row, `left` numbers inside it, at any alignment of their type
+template <typename Out>
+__device__ __forceinline__ void store_piece(Out* p, uintx4 v, int left)
+{
+    constexpr int N = 16 / sizeof(Out);
+    if (left >= N) {
+        if constexpr (sizeof(Out) == 4) *reinterpret_cast<Words4*>(p) = Words4{{v[0], v[1], v[2], v[3]}};
+        else *reinterpret_cast<Bytes16*>(p) = Bytes16{{v[0], v[1], v[2], v[3]}};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i) {
+        if constexpr (sizeof(Out) == 4) { if (i < left) p[i] = __uint_as_float(v[i]); }
+        else { if (i < left) reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(v[i >> 1] >> (16 * (i & 1))); }
+    }
+}
+
 // up to eight 16-bit numbers from an address of any alignment, zeros behind them
 __device__ __forceinline__ uintx4 fetch_some(const char* p, int count)
 {
@@ -453,11 +470,17 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
         else fa[S & 1][I == 0 ? 0 : I - TN] = A::operand(buffer, (wm * TM + (I == 0 ? 0 : I - TN)) * 32, S, lane);
     };
     const auto operands = [&](const uintx4* buffer, auto s) { static_for<0, TM + TN>([&](auto i) { operand(buffer, s, i); }); };
-    // Step S: its products in turn with the reads of the next step's operands (step `next_s`, from `next`) and with loads of chunk `c` to
-    // LDS: of operand A (LOADS 1), of B (2).  The compiler keeps to this order.
-    const auto step = [&](auto s, const uintx4* next, auto next_s, auto loads, int c, uintx4* to) {
-        constexpr int S = s.value, LOADS = ANY ? 0 : loads.value, N = TM * TN, READS = TM + TN;
-        constexpr int COUNT = LOADS == 1 ? A::kLoads : (LOADS == 2 ? B::kLoads : 0);
+    // load L of chunk `c`: those of operand A, then those of B
+    constexpr int kLoads = ANY ? 0 : A::kLoads + B::kLoads, kEarly = kLoads / 2;
+    const auto load = [&](auto l, int c, uintx4* to) {
+        constexpr int L = l.value;
+        if constexpr (L < A::kLoads) oa.template load<L>(to, a + c * step_a, depth - c * unit_a, wave, lane);
+        else ob.template load<L - A::kLoads>(to + BM * kChunkPieces, b + c * step_b, depth_b - c * unit_b, wave, lane);
+    };
+    // Step S: its products in turn with the reads of the next step's operands (step `next_s`, from `next`) and with loads FIRST to LAST of
+    // chunk `c` to LDS.  The compiler keeps to this order.
+    const auto step = [&](auto s, const uintx4* next, auto next_s, auto first, auto last, int c, uintx4* to) {
+        constexpr int S = s.value, N = TM * TN, READS = TM + TN, FIRST = first.value, COUNT = last.value - FIRST;
         static_for<0, N>([&](auto i) {
             constexpr int I = i.value, t = I / TN, u = I % TN;
             constexpr int rate = (READS + N - 1) / N;
@@ -466,10 +489,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
             const uintx4 x = fa[S & 1][t], w = fb[S & 1][u];
             if constexpr (MX) acc[t][u] = multiply32_scaled<2 * (S & 1)>(w, x, acc[t][u], S < 2 ? tb[u].x : tb[u].y, S < 2 ? ta[t].x : ta[t].y);
             else acc[t][u] = multiply32<TYPE>(w, x, acc[t][u]);
-            static_for<I * COUNT / N, (I + 1) * COUNT / N>([&](auto l) {
-                if constexpr (LOADS == 1) oa.template load<l.value>(to, a + c * step_a, depth - c * unit_a, wave, lane);
-                else if constexpr (LOADS == 2) ob.template load<l.value>(to + BM * kChunkPieces, b + c * step_b, depth_b - c * unit_b, wave, lane);
-            });
+            static_for<FIRST + I * COUNT / N, FIRST + (I + 1) * COUNT / N>([&](auto l) { load(l, c, to); });
             __builtin_amdgcn_sched_barrier(0);
         });
     };
@@ -477,6 +497,8 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
     constexpr std::integral_constant<int, 1> s1{};
     constexpr std::integral_constant<int, 2> s2{};
     constexpr std::integral_constant<int, 3> s3{};
+    constexpr std::integral_constant<int, kEarly> early{};
+    constexpr std::integral_constant<int, kLoads> all{};
     // every wave's pieces of the next chunk are in place, and the present one has been read
     const auto meet = [&] {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -487,16 +509,16 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
     // chunk come during that step too.  FIRST: first of a pair, which brings the next pair's scales.
     const auto chunk = [&](int c, uintx4* now, uintx4* next, auto first) {
         if constexpr (MX) own_scales();
-        step(s0, now, s1, s2, c + 1, next);
+        step(s0, now, s1, early, all, c + 1, next);
         if constexpr (MX && first.value) fetch_scales(c + 2);
-        step(s1, now, s2, s0, 0, nullptr);
-        step(s2, now, s3, s0, 0, nullptr);
+        step(s1, now, s2, s0, s0, 0, nullptr);
+        step(s2, now, s3, s0, s0, 0, nullptr);
         put(next);
         meet();
         fetch(c + 2);
         if constexpr (MX && first.value) put_scales(c + 2);
         if constexpr (MX) take_scales(c + 1);
-        step(s3, next, s0, s1, c + 2, now);
+        step(s3, next, s0, s0, early, c + 2, now);
     };
     // An odd number of chunks: the first by itself, out of the other buffer (4-bit operands: one of zeros behind the last).  Chunks behind the
     // last are zeros, asked for and not multiplied.
@@ -507,9 +529,8 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
             put(first);
             fetch(1);
         } else {
-            static_for<0, A::kLoads>([&](auto l) { oa.template load<l.value>(first, a, depth, wave, lane); });
-            static_for<0, B::kLoads>([&](auto l) { ob.template load<l.value>(first + BM * kChunkPieces, b, depth_b, wave, lane); });
-            static_for<0, A::kLoads>([&](auto l) { oa.template load<l.value>(second, a + step_a, depth - unit_a, wave, lane); });
+            static_for<0, kLoads>([&](auto l) { load(l, 0, first); });
+            static_for<0, kEarly>([&](auto l) { load(l, 1, second); });
         }
         if constexpr (MX) {
             fetch_scales(0);
@@ -532,20 +553,31 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
         chunk(c + 1, odd, even, s0);
     }
 
-    // result register v of lane l: column 8 (v / 4) + 4 (l / 32) + v % 4, row l % 32 of its 32 x 32 tile
-    const bool vector = p.out_stride % 4 == 0;
+    // Result register v of lane l: column 8 (v / 4) + 4 (l / 32) + v % 4, row l % 32 of its 32 x 32 tile.  Stored from there, an instruction would
+    // write 16 bytes to each of 32 rows; through LDS (a part of its own for each wave, 32 rows at a time, the 16-byte pieces of a row exchanged by
+    // its number) they are whole runs of 32 TN columns.
+    meet();
+    constexpr int kOutPieces = TN * 32 * (int)sizeof(Out) / 16, kPieceOuts = 16 / (int)sizeof(Out);
+    static_assert(WAVES * 32 * kOutPieces <= (BM + BN) * kChunkPieces, "fits a buffer");
+    uintx4* mine = even + wave * 32 * kOutPieces;
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
-        const int r = (wm * TM + t) * 32 + (lane & 31);
-        if (r >= m_rows) continue;
-        Out* row = out + r * p.out_stride;
 #pragma unroll
         for (int u = 0; u < TN; ++u)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int col = (wn * TN + u) * 32 + 8 * q + 4 * (lane >> 5);
-                store_four(row + col, acc[t][u][4 * q], acc[t][u][4 * q + 1], acc[t][u][4 * q + 2], acc[t][u][4 * q + 3], cols_left - col, vector);
+                const int r = lane & 31, col = u * 32 + 8 * q + 4 * (lane >> 5), piece = (col / kPieceOuts) ^ (r & (kOutPieces - 1));
+                const float *v = reinterpret_cast<const float*>(&acc[t][u]) + 4 * q;
+                if constexpr (sizeof(Out) == 4) mine[r * kOutPieces + piece] = uintx4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                else reinterpret_cast<uint2*>(mine + r * kOutPieces + piece)[lane >> 5] = uint2{Piece<Out>::narrow(v[0], v[1]), Piece<Out>::narrow(v[2], v[3])};
             }
+#pragma unroll
+        for (int k = 0; k < 32 * kOutPieces / 64; ++k) {
+            const int r = k * (64 / kOutPieces) + lane / kOutPieces, piece = lane % kOutPieces;
+            const uintx4 v = mine[r * kOutPieces + (piece ^ (r & (kOutPieces - 1)))];
+            const int row = (wm * TM + t) * 32 + r, col = wn * TN * 32 + piece * kPieceOuts;
+            if (row < m_rows) store_piece(out + row * p.out_stride + col, v, cols_left - col);
+        }
     }
 }
 
