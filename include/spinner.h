@@ -482,7 +482,10 @@ int spinner_mx_linear(const void *x, int dtype, long rows, int k, long x_stride,
  * are made of whole 16-byte pieces (k, n and the strides multiples of 8) take
  * the faster way.  dw is overwritten, zeros for an expert without rows, in fp32
  * or in the type of dy and x (dw_dtype).  Rows of no expert: 0 in out and dx,
- * and not in dw.  Strides as above.
+ * and not in dw.  Strides as above.  spinner_grouped_matmul_dw: few results with
+ * many rows are summed up in shares, workspace then holds
+ * spinner_grouped_matmul_dw_workspace_bytes(rows, n, k, experts) bytes (NULL when
+ * that is 0).  All sums are made in an order that the sizes alone decide.
  */
 int spinner_grouped_matmul(const void *x, int dtype, long rows, int k, long x_stride,
                            const void *w, int n, int experts, const long long *ends,
@@ -492,7 +495,8 @@ int spinner_grouped_matmul_dx(const void *dy, int dtype, long rows, int n, long 
                               void *dx, long dx_stride, void *stream);
 int spinner_grouped_matmul_dw(const void *dy, const void *x, int dtype, long rows, int n, int k,
                               long dy_stride, long x_stride, int experts, const long long *ends,
-                              void *dw, int dw_dtype, void *stream);
+                              void *dw, int dw_dtype, void *workspace, void *stream);
+size_t spinner_grouped_matmul_dw_workspace_bytes(long rows, int n, int k, int experts);
 
 /*
  * Bytes of device scratch spinner_apply needs for these arguments: 0 up to the

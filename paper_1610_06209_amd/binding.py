@@ -44,7 +44,8 @@ EXPORTS = ["spinner_apply", "spinner_hash", "spinner_workspace_bytes", "spinner_
            "spinner_struct_params", "spinner_struct_spectrum_bytes", "spinner_struct_prepare", "spinner_struct_apply",
            "spinner_struct_workspace_bytes", "spinner_struct_apply_ws",
            "spinner_mx_quantize", "spinner_mx_dequantize", "spinner_mx_matmul", "spinner_mx_linear_workspace_bytes",
-           "spinner_mx_linear", "spinner_grouped_matmul", "spinner_grouped_matmul_dx", "spinner_grouped_matmul_dw"]
+           "spinner_mx_linear", "spinner_grouped_matmul", "spinner_grouped_matmul_dx", "spinner_grouped_matmul_dw",
+           "spinner_grouped_matmul_dw_workspace_bytes"]
 
 if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_native.so")):
     raise ImportError(
@@ -158,7 +159,9 @@ lib.spinner_grouped_matmul.argtypes = [_vp, _int, _long, _int, _long, _vp, _int,
 lib.spinner_grouped_matmul_dx.restype = _int
 lib.spinner_grouped_matmul_dx.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _int, _vp, _vp, _long, _vp]
 lib.spinner_grouped_matmul_dw.restype = _int
-lib.spinner_grouped_matmul_dw.argtypes = [_vp, _vp, _int, _long, _int, _int, _long, _long, _int, _vp, _vp, _int, _vp]
+lib.spinner_grouped_matmul_dw.argtypes = [_vp, _vp, _int, _long, _int, _int, _long, _long, _int, _vp, _vp, _int, _vp, _vp]
+lib.spinner_grouped_matmul_dw_workspace_bytes.restype = ctypes.c_size_t
+lib.spinner_grouped_matmul_dw_workspace_bytes.argtypes = [_long, _int, _int, _int]
 STRUCT_KINDS = {"circulant": 0, "skew_circulant": 1, "toeplitz": 2, "hankel": 3}
 
 
@@ -1025,12 +1028,16 @@ def spinner_grouped_matmul_dx(dy, w, ends=None, dx=None, stream=None):
     return r if r is not None else _grouped(lib.spinner_grouped_matmul_dx, dy, w, ends, dx, stream, False)
 
 
-def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, stream=None):
+def spinner_grouped_matmul_dw_workspace_bytes(rows: int, n: int, k: int, experts: int) -> int:
+    return int(lib.spinner_grouped_matmul_dw_workspace_bytes(int(rows), int(n), int(k), int(experts)))
+
+
+def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, workspace=None, stream=None):
     """Gradient with respect to w: dw = dy^T x over each expert's rows, [experts][n][k] ([n][k] without ends).
 
     dtype: fp32, or the type of dy and x.  Experts without rows get zeros.
     """
-    r = _native.grouped_matmul_dw(dy, x, ends, dtype, dw, stream)
+    r = _native.grouped_matmul_dw(dy, x, ends, dtype, dw, workspace, stream)
     if r is not None:
         return r
     dy_stride, x_stride = _check_rows(dy, "dy"), _check_rows(x, "x", dy.dtype)
@@ -1041,13 +1048,17 @@ def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, st
     experts = 1 if ends is None else ends.numel()
     e = _check_ends(ends, experts, "dw")
     shape = (n, k) if ends is None else (experts, n, k)
-    made = dw is None
-    if made:
+    made = dw is None, workspace is None
+    if dw is None:
         dw = torch.empty(shape, dtype=dtype, device=dy.device)
     _check_here(dw, "dw", dtype)
     if tuple(dw.shape) != shape or not dw.is_contiguous():
         raise ValueError("dw must be contiguous, of shape %s" % (shape,))
+    need = spinner_grouped_matmul_dw_workspace_bytes(rows, n, k, experts)
+    if need and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+    _check_workspace(workspace, need)
     _done(lib.spinner_grouped_matmul_dw(dy.data_ptr(), x.data_ptr(), code, rows, n, k, dy_stride, x_stride, experts, e, dw.data_ptr(), dw_code,
-                                        _stream_handle(stream)))
-    _in_use(stream, dw if made else None)
+                                        workspace.data_ptr() if workspace is not None else None, _stream_handle(stream)))
+    _in_use(stream, dw if made[0] else None, workspace if made[1] else None)
     return dw

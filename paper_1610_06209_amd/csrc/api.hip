@@ -967,6 +967,7 @@ int spinner_mx_matmul(const void* a_codes, const void* a_scales, long rows, int 
     p.experts = experts;
     p.width = n;
     p.depth = k;
+    spinner::plan_product(spinner::kForward, true, &p);
     return launched(spinner::launch_product_mx4(dtype, p, static_cast<hipStream_t>(stream)));
 }
 
@@ -1020,6 +1021,7 @@ static int grouped(int direction, const void* a, int dtype, long rows, long a_st
     p.experts = experts;
     p.width = forward ? n : k;
     p.depth = forward ? k : n;
+    spinner::plan_product(direction, false, &p);
     const auto launch = dtype == SPINNER_BF16 ? spinner::launch_product_bf16 : spinner::launch_product_f16;
     return launched(launch(direction, dtype, p, static_cast<hipStream_t>(stream)));
 }
@@ -1036,27 +1038,42 @@ int spinner_grouped_matmul_dx(const void* dy, int dtype, long rows, int n, long 
     return grouped(spinner::kDx, dy, dtype, rows, dy_stride, w, n, k, experts, ends, dx, dx_stride, stream);
 }
 
+static spinner::ProductParams dw_params(long rows, int n, int k, int experts, const long long* ends)
+{
+    spinner::ProductParams p = {};
+    p.ends = ends;
+    p.out_stride = k;
+    p.rows = (int)rows;
+    p.experts = experts;
+    p.height = n;
+    p.width = k;
+    spinner::plan_product(spinner::kDw, false, &p);
+    return p;
+}
+
+size_t spinner_grouped_matmul_dw_workspace_bytes(long rows, int n, int k, int experts)
+{
+    if (rows < 0 || rows > 0x7fffffffL || experts < 1 || experts > spinner::kMaxExperts || !side(n) || !side(k)) return 0;
+    return spinner::product_workspace(dw_params(rows, n, k, experts, nullptr));
+}
+
 int spinner_grouped_matmul_dw(const void* dy, const void* x, int dtype, long rows, int n, int k, long dy_stride, long x_stride,
-                              int experts, const long long* ends, void* dw, int dw_dtype, void* stream)
+                              int experts, const long long* ends, void* dw, int dw_dtype, void* workspace, void* stream)
 {
     if (!type16(dtype) || (dw_dtype != dtype && dw_dtype != SPINNER_F32)) return SPINNER_ERR_BAD_TYPE;
     const int rc = check_groups(rows, experts, ends);
     if (rc != SPINNER_OK) return rc;
     if (!side(n) || !side(k) || !stride_in(dy_stride) || !stride_in(x_stride)) return SPINNER_ERR_BAD_SHAPE;
     if ((rows && (!dy || !x)) || !dw) return SPINNER_ERR_NULL_PTR;
-    if (!aligned16(dy) || !aligned16(x) || !aligned16(dw)) return SPINNER_ERR_ALIGNMENT;
-    spinner::ProductParams p = {};
+    spinner::ProductParams p = dw_params(rows, n, k, experts, ends);
+    if (product_workspace(p) && !workspace) return SPINNER_ERR_WORKSPACE;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(dw) || !aligned16(workspace)) return SPINNER_ERR_ALIGNMENT;
     p.a = static_cast<const char*>(dy);
     p.b = static_cast<const char*>(x);
     p.out = static_cast<char*>(dw);
-    p.ends = ends;
     p.a_stride = 2LL * dy_stride;
     p.b_stride = 2LL * x_stride;
-    p.out_stride = k;
-    p.rows = (int)rows;
-    p.experts = experts;
-    p.height = n;
-    p.width = k;
+    p.workspace = workspace;
     const auto launch = dtype == SPINNER_BF16 ? spinner::launch_product_bf16 : spinner::launch_product_f16;
     return launched(launch(spinner::kDw, dw_dtype, p, static_cast<hipStream_t>(stream)));
 }

@@ -658,14 +658,14 @@ ENTRY(grouped_matmul_dx, 5)
     return grouped(a, false);
 ENTRY_END
 
-// dy, x, ends, dtype, dw, stream
-ENTRY(grouped_matmul_dw, 6)
+// dy, x, ends, dtype, dw, workspace, stream
+ENTRY(grouped_matmul_dw, 7)
     long count, x_count;
     int n, k, code, x_code, dw_code, experts = 1;
     at::ScalarType type;
     const long long* ends = nullptr;
     const Tensor *dy = number_rows(a[0], &count, &n, &code), *x = number_rows(a[1], &x_count, &k, &x_code), *given = nullptr;
-    if (!dy || !x || a[5] != Py_None || x_count != count || x_code != code || !dtype_of(a[3], &type, &dw_code)) LONG_WAY;
+    if (!dy || !x || a[6] != Py_None || x_count != count || x_code != code || !dtype_of(a[3], &type, &dw_code)) LONG_WAY;
     if (a[2] != Py_None) {
         const Tensor* e = typed_tensor(a[2], at::kLong);
         if (!e || e->dim() != 1 || e->numel() < 1 || e->numel() > INT_MAX) LONG_WAY;
@@ -677,12 +677,17 @@ ENTRY(grouped_matmul_dw, 6)
         given = typed_tensor(a[4], type);
         if (!given || given->sizes() != at::IntArrayRef(sizes)) LONG_WAY;
     }
+    const size_t need = spinner_grouped_matmul_dw_workspace_bytes(count, n, k, experts);
+    Buffer w;
+    if (!w.usable_bytes(a[5], need)) LONG_WAY;
     Tensor dw;
     int rc;
     {
         pybind11::gil_scoped_release free;
         dw = result(given, sizes, type, *dy);
-        rc = spinner_grouped_matmul_dw(ptr<void>(dy), ptr<void>(x), code, count, n, k, n, k, experts, ends, ptr<void>(dw), dw_code, current_stream());
+        const Tensor scratch = w.scratch(need, *dy);
+        rc = spinner_grouped_matmul_dw(ptr<void>(dy), ptr<void>(x), code, count, n, k, n, k, experts, ends, ptr<void>(dw), dw_code, ptr<void>(scratch),
+                                       current_stream());
     }
     if (rc != SPINNER_OK) return refused(rc);
     return THPVariable_Wrap(std::move(dw));

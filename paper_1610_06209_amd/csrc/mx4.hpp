@@ -44,7 +44,21 @@ struct ProductParams {
     int height;                           // kDw: rows of one expert's result
     int width;                            // columns of the result
     int depth;                            // kForward, kDx: numbers in a sum
+    int tile;                             // form of the kernel, see plan_product
+    int splits;                           // shares of the depth that workgroups of their own sum up (kDw; 1: whole sums)
+    long long split_stride;               // (kernels) numbers from one share's partial results to the next
+    void* workspace;                      // fp32 [splits][rows of the result][width], splits > 1
 };
+// Forms of the product: a few rows a group; tiles of 256 x 256, 128 x 128 with two or four chunks in LDS, 64 x 64.
+enum { kFewRows, kTile256, kTile128, kTile128Deep, kTile64 };
+// The form (and, kDw, the shares of the depth) that takes the shortest by what was measured of each: p.tile and p.splits.  It goes by the sizes alone: the
+// rows of each expert are known on the GPU only.
+void plan_product(int direction, bool mx4, ProductParams* p);
+inline size_t product_workspace(const ProductParams& p)      // bytes of partial sums, kDw
+{
+    return p.splits > 1 ? (size_t)p.splits * p.experts * p.height * p.width * sizeof(float) : 0;
+}
+
 hipError_t launch_product_mx4(int out_type, const ProductParams& p, hipStream_t s);           // kForward
 hipError_t launch_product_bf16(int direction, int out_type, const ProductParams& p, hipStream_t s);
 hipError_t launch_product_f16(int direction, int out_type, const ProductParams& p, hipStream_t s);

@@ -195,6 +195,7 @@ constexpr int kChunkBytes = 128;                          // of a row's depth in
 constexpr int kChunkPieces = kChunkBytes / 16;
 constexpr int kChunkDepth16 = kChunkBytes / 2;            // the same in 16-bit numbers
 constexpr int kChunkScales = kChunkBytes / 16;            // scales of a row's chunk: 32 numbers are 16 bytes
+constexpr int kHeldScales = 256;                          // most scales of a row that a tile holds at once: a depth of 8192
 constexpr unsigned kFar = 0x80000000u;                    // offsets of a tile's pieces stay below this
 
 // 16 bytes a lane from a buffer of kFar bytes at `from`, to 1 KiB of LDS.  Written out because the compiler, which counts these
@@ -321,16 +322,23 @@ struct RowScales {
     }
 };
 
-// BM x BN results a workgroup of WM x WN waves.  ANY: operands whose rows are not made of whole aligned pieces of 16 bytes.
-template <int DIRECTION, int TYPE, int BM, int BN, int WM, int WN, bool ANY, typename Out>
-__global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) product_kernel(ProductParams p)
+// BM x BN results a workgroup of WM x WN waves, STAGES chunks in LDS.  ANY: operands whose rows are not made of whole aligned pieces of
+// 16 bytes.
+template <int DIRECTION, int TYPE, int BM, int BN, int WM, int WN, int STAGES, bool ANY, typename Out>
+__global__ void __launch_bounds__(64 * WM * WN, (BM + BN) * kChunkBytes * STAGES > 80 * 1024 ? 1 : 2) product_kernel(ProductParams p)
 {
+    static_assert(STAGES == 2 || !ANY, "loads through registers are one chunk ahead");
+    // scales: two chunks' at a time, brought through registers a pair of chunks ahead; with more stages, where a wait for those would be one for
+    // all chunks on their way, all of the depth's at the start
+    constexpr bool HELD = TYPE == kMx4 && STAGES > 2;
+    constexpr int kScalePieces = HELD ? kHeldScales / 16 + 1 : 1;      // 16-byte pieces from one row's to the next in LDS
     constexpr int WAVES = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr bool MX = TYPE == kMx4;
     using A = TileOperand<DIRECTION != kDw, BM, WAVES, ANY>;
     using B = TileOperand<DIRECTION == kForward, BN, WAVES, ANY>;
-    __shared__ uintx4 even[(BM + BN) * kChunkPieces], odd[(BM + BN) * kChunkPieces];
-    __shared__ uintx4 row_scales[MX ? 2 : 1][MX ? BM + BN : 1];
+    constexpr int kBuffer = (BM + BN) * kChunkPieces, kSums = TM * TN == 1 ? 4 * 4 * 256 : 0;      // sums of the four waves of 64 x 64
+    __shared__ uintx4 buffers[STAGES * kBuffer > kSums ? STAGES * kBuffer : kSums];
+    __shared__ uintx4 row_scales[MX ? (HELD ? 1 : 2) : 1][MX ? (BM + BN) * kScalePieces : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const unsigned columns = (unsigned)(p.width + BN - 1) / BN;
@@ -408,10 +416,20 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
 
     // depth in units of an operand: bytes along deep rows, rows of flat ones
     constexpr int unit_a = DIRECTION == kDw ? kChunkDepth16 : kChunkBytes, unit_b = DIRECTION == kForward ? kChunkBytes : kChunkDepth16;
-    const int depth_b = DIRECTION == kDx ? depth / 2 : depth;
-    const int chunks = (depth + unit_a - 1) / unit_a;
     const long long step_a = DIRECTION == kDw ? kChunkDepth16 * p.a_stride : kChunkBytes;
     const long long step_b = DIRECTION == kForward ? kChunkBytes : kChunkDepth16 * p.b_stride;
+    int chunks = (depth + unit_a - 1) / unit_a;
+    if constexpr (DIRECTION == kDw)
+        if (p.splits > 1) {                   // this workgroup's share of the depth, and its place among the partial sums
+            const int share = (chunks + p.splits - 1) / p.splits, first = share * (int)blockIdx.y;
+            a += first * step_a;
+            b += first * step_b;
+            depth -= first * unit_a;
+            depth = depth < 0 ? 0 : (depth < share * unit_a ? depth : share * unit_a);
+            chunks = (depth + unit_a - 1) / unit_a;
+            out += blockIdx.y * p.split_stride;
+        }
+    const int depth_b = DIRECTION == kDx ? depth / 2 : depth;
 
     uintx4 va[ANY ? A::kLoads : 1], vb[ANY ? B::kLoads : 1];
     const auto fetch = [&](int c) {
@@ -428,30 +446,38 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
     };
     // Scales (kMx4): every thread brings those of some rows for a pair of chunks; a lane takes the eight bytes of its rows for one chunk, shifted
     // so that its own of each step's two is byte 0 or 2.
-    constexpr int THREADS = 64 * WAVES, kScaleRows = MX ? (BM + BN) / THREADS : 1;
-    static_assert(!MX || (BM % THREADS == 0 || THREADS % BM == 0) && (BM + BN) % THREADS == 0, "whole rows a thread");
+    constexpr int THREADS = 64 * WAVES, kScaleRows = MX ? (BM + BN + THREADS - 1) / THREADS : 1;
     const int scale_count = MX ? p.depth / kMx4Block : 0;
     RowScales brought[kScaleRows];
     const auto fetch_scales = [&](int c) {
 #pragma unroll
         for (int i = 0; i < kScaleRows; ++i) {
             const int r = i * THREADS + (int)threadIdx.x;
+            if ((BM + BN) % THREADS && r >= BM + BN) break;
             const int ra = r < rows_left ? r : rows_left - 1, rb = r - BM < cols_left ? r - BM : cols_left - 1;
             const unsigned at = (unsigned)((r < BM ? ra : rb) * scale_count + c * kChunkScales);
             brought[i].fetch(r < BM ? a_scales : b_scales, at, r < BM ? a_end : b_end);
         }
     };
-    const auto put_scales = [&](int c) {
+    const auto put_scales = [&](int c) {      // HELD: the pair's place in its row
 #pragma unroll
-        for (int i = 0; i < kScaleRows; ++i) brought[i].put(&row_scales[c >> 1 & 1][i * THREADS + threadIdx.x], scale_count - c * kChunkScales);
+        for (int i = 0; i < kScaleRows; ++i) {
+            const int r = i * THREADS + (int)threadIdx.x;
+            if ((BM + BN) % THREADS && r >= BM + BN) break;
+            brought[i].put(HELD ? &row_scales[0][r * kScalePieces + (c >> 1)] : &row_scales[c >> 1 & 1][r], scale_count - c * kChunkScales);
+        }
+    };
+    const auto scale_piece = [&](int c, int r) -> const uintx4* {
+        return HELD ? &row_scales[0][r * kScalePieces + (c >> 1)] : &row_scales[c >> 1 & 1][r];
     };
     uint2 sa[MX ? TM : 1], sb[MX ? TN : 1];
     const auto take_scales = [&](int c) {
-        const char* from = reinterpret_cast<const char*>(&row_scales[c >> 1 & 1][lane & 31]) + (c & 1) * kChunkScales;
+        const char* from = reinterpret_cast<const char*>(scale_piece(c, lane & 31)) + (c & 1) * kChunkScales;
+        constexpr int row = kScalePieces * 16;
 #pragma unroll
-        for (int t = 0; t < TM; ++t) sa[t] = *reinterpret_cast<const uint2*>(from + (wm * TM + t) * 32 * 16);
+        for (int t = 0; t < TM; ++t) sa[t] = *reinterpret_cast<const uint2*>(from + (wm * TM + t) * 32 * row);
 #pragma unroll
-        for (int u = 0; u < TN; ++u) sb[u] = *reinterpret_cast<const uint2*>(from + (BM + (wn * TN + u) * 32) * 16);
+        for (int u = 0; u < TN; ++u) sb[u] = *reinterpret_cast<const uint2*>(from + (BM + (wn * TN + u) * 32) * row);
     };
     uint2 ta[MX ? TM : 1], tb[MX ? TN : 1];
     const auto own_scales = [&] {
@@ -462,104 +488,190 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
         for (int u = 0; u < TN; ++u) tb[u] = {sb[u].x >> shift, sb[u].y >> shift};
     };
 
-    uintx4 fa[2][TM], fb[2][TN];
-    // operand I of step S: the first rows' and all columns' come first, as they are multiplied
-    const auto operand = [&](const uintx4* buffer, auto s, auto i) {
-        constexpr int S = s.value, I = i.value;
-        if constexpr (I >= 1 && I <= TN) fb[S & 1][I - 1] = B::operand(buffer + BM * kChunkPieces, (wn * TN + I - 1) * 32, S, lane);
-        else fa[S & 1][I == 0 ? 0 : I - TN] = A::operand(buffer, (wm * TM + (I == 0 ? 0 : I - TN)) * 32, S, lane);
-    };
-    const auto operands = [&](const uintx4* buffer, auto s) { static_for<0, TM + TN>([&](auto i) { operand(buffer, s, i); }); };
     // load L of chunk `c`: those of operand A, then those of B
-    constexpr int kLoads = ANY ? 0 : A::kLoads + B::kLoads, kEarly = kLoads / 2;
+    constexpr int kLoads = ANY ? 0 : A::kLoads + B::kLoads;
     const auto load = [&](auto l, int c, uintx4* to) {
         constexpr int L = l.value;
         if constexpr (L < A::kLoads) oa.template load<L>(to, a + c * step_a, depth - c * unit_a, wave, lane);
         else ob.template load<L - A::kLoads>(to + BM * kChunkPieces, b + c * step_b, depth_b - c * unit_b, wave, lane);
     };
-    // Step S: its products in turn with the reads of the next step's operands (step `next_s`, from `next`) and with loads FIRST to LAST of
-    // chunk `c` to LDS.  The compiler keeps to this order.
-    const auto step = [&](auto s, const uintx4* next, auto next_s, auto first, auto last, int c, uintx4* to) {
-        constexpr int S = s.value, N = TM * TN, READS = TM + TN, FIRST = first.value, COUNT = last.value - FIRST;
-        static_for<0, N>([&](auto i) {
-            constexpr int I = i.value, t = I / TN, u = I % TN;
-            constexpr int rate = (READS + N - 1) / N;
-            static_for<I * rate, (I + 1) * rate < READS ? (I + 1) * rate : READS>([&](auto r) { operand(next, next_s, r); });
-            // columns of the result along the instruction's rows: a lane then holds four neighbours of a row of `out`
-            const uintx4 x = fa[S & 1][t], w = fb[S & 1][u];
-            if constexpr (MX) acc[t][u] = multiply32_scaled<2 * (S & 1)>(w, x, acc[t][u], S < 2 ? tb[u].x : tb[u].y, S < 2 ? ta[t].x : ta[t].y);
-            else acc[t][u] = multiply32<TYPE>(w, x, acc[t][u]);
-            static_for<FIRST + I * COUNT / N, FIRST + (I + 1) * COUNT / N>([&](auto l) { load(l, c, to); });
-            __builtin_amdgcn_sched_barrier(0);
-        });
+    const auto multiply = [&](auto s, auto t, auto u, uintx4 x, uintx4 w) {
+        constexpr int S = s.value, T = t.value, U = u.value;
+        // columns of the result along the instruction's rows: a lane then holds four neighbours of a row of `out`
+        if constexpr (MX) acc[T][U] = multiply32_scaled<2 * (S & 1)>(w, x, acc[T][U], S < 2 ? tb[U].x : tb[U].y, S < 2 ? ta[T].x : ta[T].y);
+        else acc[T][U] = multiply32<TYPE>(w, x, acc[T][U]);
+    };
+    // This wave's loads are in place but for the last `on_their_way`, and what it asked LDS for has arrived; so it is for all waves.
+    const auto meet = [&](auto on_their_way) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(on_their_way.value) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
     };
     constexpr std::integral_constant<int, 0> s0{};
     constexpr std::integral_constant<int, 1> s1{};
     constexpr std::integral_constant<int, 2> s2{};
     constexpr std::integral_constant<int, 3> s3{};
-    constexpr std::integral_constant<int, kEarly> early{};
-    constexpr std::integral_constant<int, kLoads> all{};
-    // every wave's pieces of the next chunk are in place, and the present one has been read
-    const auto meet = [&] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    // A chunk is four steps, the operands of each read while the one before is multiplied.  Its last operands are read before the
-    // waves meet, so that its buffer is free for the chunk after the next from its last step on, and the first operands of the next
-    // chunk come during that step too.  FIRST: first of a pair, which brings the next pair's scales.
-    const auto chunk = [&](int c, uintx4* now, uintx4* next, auto first) {
-        if constexpr (MX) own_scales();
-        step(s0, now, s1, early, all, c + 1, next);
-        if constexpr (MX && first.value) fetch_scales(c + 2);
-        step(s1, now, s2, s0, s0, 0, nullptr);
-        step(s2, now, s3, s0, s0, 0, nullptr);
-        put(next);
-        meet();
-        fetch(c + 2);
-        if constexpr (MX && first.value) put_scales(c + 2);
-        if constexpr (MX) take_scales(c + 1);
-        step(s3, next, s0, s0, early, c + 2, now);
-    };
-    // An odd number of chunks: the first by itself, out of the other buffer (4-bit operands: one of zeros behind the last).  Chunks behind the
-    // last are zeros, asked for and not multiplied.
-    const bool lone = !MX && (chunks & 1);
-    const auto begin = [&](uintx4* first, uintx4* second) {
-        if constexpr (ANY) {
-            fetch(0);
-            put(first);
-            fetch(1);
-        } else {
-            static_for<0, kLoads>([&](auto l) { load(l, 0, first); });
-            static_for<0, kEarly>([&](auto l) { load(l, 1, second); });
+    constexpr std::integral_constant<int, (STAGES - 2) * kLoads> behind{};
+    int at = 0;                    // buffer of the chunk at hand
+    // Chunks behind the last are zeros: they are asked for, and not multiplied but for one that makes 4-bit chunks pairs.
+    fetch(0);
+    put(buffers);
+    fetch(1);
+    static_for<0, STAGES - 1>([&](auto k) { static_for<0, kLoads>([&](auto l) { load(l, k.value, buffers + k.value * kBuffer); }); });
+    if constexpr (HELD) {
+        // one pair of chunks of a row a thread at a time
+        const int pairs = (chunks + 1) / 2, count = pairs * (BM + BN);
+        for (int k = threadIdx.x; k < count; k += THREADS) {
+            const int r = k / pairs, pair = k - r * pairs;
+            const int ra = r < rows_left ? r : rows_left - 1, rb = r - BM < cols_left ? r - BM : cols_left - 1;
+            RowScales v;
+            v.fetch(r < BM ? a_scales : b_scales, (unsigned)((r < BM ? ra : rb) * scale_count + pair * 16), r < BM ? a_end : b_end);
+            v.put(&row_scales[0][r * kScalePieces + pair], scale_count - pair * 16);
         }
-        if constexpr (MX) {
-            fetch_scales(0);
-            put_scales(0);
-        }
-        meet();
+    } else if constexpr (MX) {
+        fetch_scales(0);
+        put_scales(0);
+    }
+    if constexpr (TM * TN > 1) {
+        // A chunk is four steps, the operands of each read while the one before is multiplied.  A chunk's last
+        // operands are read before the waves meet, so that its buffer is free for a later chunk from its last step on, and the first operands
+        // of the next chunk come during that step too.  The loads of a chunk are spread over two steps.
+        constexpr int kEarly = kLoads / 2;
+        constexpr std::integral_constant<int, kEarly> early{};
+        constexpr std::integral_constant<int, kLoads> all{};
+        uintx4 fa[2][TM], fb[2][TN];
+        // operand I of step S: the first rows' and all columns' come first, as they are multiplied
+        const auto operand = [&](const uintx4* buffer, auto s, auto i) {
+            constexpr int S = s.value, I = i.value;
+            if constexpr (I >= 1 && I <= TN) fb[S & 1][I - 1] = B::operand(buffer + BM * kChunkPieces, (wn * TN + I - 1) * 32, S, lane);
+            else fa[S & 1][I == 0 ? 0 : I - TN] = A::operand(buffer, (wm * TM + (I == 0 ? 0 : I - TN)) * 32, S, lane);
+        };
+        // Step S: its products in turn with the reads of the next step's operands (step `next_s`, from `next`) and with loads FIRST to LAST
+        // of chunk `c` to LDS.  The compiler keeps to this order.
+        const auto step = [&](auto s, const uintx4* next, auto next_s, auto first, auto last, int c, uintx4* to) {
+            constexpr int S = s.value, N = TM * TN, READS = TM + TN, FIRST = first.value, COUNT = last.value - FIRST;
+            static_for<0, N>([&](auto i) {
+                constexpr int I = i.value, t = I / TN, u = I % TN;
+                constexpr int rate = (READS + N - 1) / N;
+                static_for<I * rate, (I + 1) * rate < READS ? (I + 1) * rate : READS>([&](auto r) { operand(next, next_s, r); });
+                multiply(s, std::integral_constant<int, t>{}, std::integral_constant<int, u>{}, fa[S & 1][t], fb[S & 1][u]);
+                static_for<FIRST + I * COUNT / N, FIRST + (I + 1) * COUNT / N>([&](auto l) { load(l, c, to); });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        const auto chunk = [&](int c, auto first) {      // first: of a pair, which brings the next pair's scales
+            uintx4* now = buffers + at * kBuffer;
+            uintx4* last = buffers + (at ? at - 1 : STAGES - 1) * kBuffer;      // of the chunk before, the first to be free
+            at = at + 1 < STAGES ? at + 1 : 0;
+            uintx4* next = buffers + at * kBuffer;
+            if constexpr (MX) own_scales();
+            step(s0, now, s1, early, all, c + STAGES - 1, last);
+            if constexpr (MX && !HELD && first.value) fetch_scales(c + 2);
+            step(s1, now, s2, s0, s0, 0, nullptr);
+            step(s2, now, s3, s0, s0, 0, nullptr);
+            put(next);
+            meet(behind);
+            fetch(c + 2);
+            if constexpr (MX && !HELD && first.value) put_scales(c + 2);
+            if constexpr (MX) take_scales(c + 1);
+            step(s3, next, s0, s0, early, c + STAGES, now);
+        };
+        static_for<0, kEarly>([&](auto l) { load(l, STAGES - 1, buffers + (STAGES - 1) * kBuffer); });
+        meet(std::integral_constant<int, (STAGES - 2) * kLoads + kEarly>{});
         if constexpr (MX) take_scales(0);
-        operands(first, s0);
-    };
-    int c = 0;
-    if (lone) {
-        begin(odd, even);
-        chunk(0, odd, even, s0);
-        c = 1;
+        static_for<0, TM + TN>([&](auto i) { operand(buffers, s0, i); });
+        for (int c = 0; c < chunks; ++c) {
+            chunk(c, s1);
+            if constexpr (MX) chunk(++c, s0);
+        }
     } else {
-        begin(even, odd);
+        // 64 x 64: a wave that multiplied a quarter of the tile would read two operands of LDS a product.  Here each multiplies the whole tile, one
+        // step of a chunk's four each, four products for four operands, read while those of the chunk before are multiplied; the four
+        // sums meet at the end.
+        static_assert(BM == 64 && BN == 64 && WAVES == 4, "a quarter of the result a wave");
+        uintx4 fa[2][2], fb[2][2];
+        floatx16 sum[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) sum[t][u] = acc[0][0];
+        const auto operands = [&](const uintx4* buffer, auto set) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) fa[set.value][t] = A::operand(buffer, t * 32, wave, lane);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) fb[set.value][u] = B::operand(buffer + BM * kChunkPieces, u * 32, wave, lane);
+        };
+        unsigned xa[2], xb[2], ya[2], yb[2];          // scales of the wave's step: as read, and shifted so that the lane's own is byte 0
+        const auto take = [&](int c) {
+            const int word = (c & 1) * 2 + (wave >> 1), r = lane & 31;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                xa[t] = reinterpret_cast<const unsigned*>(scale_piece(c, t * 32 + r))[word];
+                xb[t] = reinterpret_cast<const unsigned*>(scale_piece(c, BM + t * 32 + r))[word];
+            }
+        };
+        const auto chunk = [&](int c, auto set) {
+            uintx4* now = buffers + at * kBuffer;
+            at = at + 1 < STAGES ? at + 1 : 0;
+            uintx4* next = buffers + at * kBuffer;
+            put(next);
+            if constexpr (MX && !HELD && set.value == 1) put_scales(c + 1);
+            meet(behind);
+            if constexpr (MX) {
+                const int shift = (lane >> 5) * 8 + (wave & 1) * 16;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) { ya[t] = xa[t] >> shift; yb[t] = xb[t] >> shift; }
+            }
+            fetch(c + 2);
+            if constexpr (MX && !HELD && set.value == 0) fetch_scales(c + 2);
+            operands(next, std::integral_constant<int, 1 - set.value>{});
+            if constexpr (MX) take(c + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<0, 4>([&](auto i) {
+                constexpr int t = i.value / 2, u = i.value % 2;
+                if constexpr (MX) sum[t][u] = multiply32_scaled<0>(fb[set.value][u], fa[set.value][t], sum[t][u], yb[u], ya[t]);
+                else sum[t][u] = multiply32<TYPE>(fb[set.value][u], fa[set.value][t], sum[t][u]);
+                static_for<i.value * kLoads / 4, (i.value + 1) * kLoads / 4>([&](auto l) { load(l, c + STAGES, now); });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        static_for<0, kLoads>([&](auto l) { load(l, STAGES - 1, buffers + (STAGES - 1) * kBuffer); });
+        meet(std::integral_constant<int, (STAGES - 1) * kLoads>{});
+        if constexpr (MX) take(0);
+        operands(buffers, s0);
+        for (int c = 0; c < chunks; c += 2) {
+            chunk(c, s0);
+            if (!MX && c + 1 >= chunks) break;
+            chunk(c + 1, s1);
+        }
+        meet(s0);
+        floatx4* part = reinterpret_cast<floatx4*>(buffers);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    part[((wave * 4 + t * 2 + u) * 4 + q) * 64 + lane] = floatx4{sum[t][u][4 * q], sum[t][u][4 * q + 1], sum[t][u][4 * q + 2], sum[t][u][4 * q + 3]};
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            floatx4 v[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[w] = part[((w * 4 + wave) * 4 + q) * 64 + lane];
+            const floatx4 all = (v[0] + v[1]) + (v[2] + v[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[0][0][4 * q + k] = all[k];
+        }
     }
-    for (; c < chunks; c += 2) {
-        chunk(c, even, odd, s1);
-        chunk(c + 1, odd, even, s0);
-    }
+    meet(s0);
 
     // Result register v of lane l: column 8 (v / 4) + 4 (l / 32) + v % 4, row l % 32 of its 32 x 32 tile.  Stored from there, an instruction would
     // write 16 bytes to each of 32 rows; through LDS (a part of its own for each wave, 32 rows at a time, the 16-byte pieces of a row exchanged by
     // its number) they are whole runs of 32 TN columns.
-    meet();
     constexpr int kOutPieces = TN * 32 * (int)sizeof(Out) / 16, kPieceOuts = 16 / (int)sizeof(Out);
-    static_assert(WAVES * 32 * kOutPieces <= (BM + BN) * kChunkPieces, "fits a buffer");
-    uintx4* mine = even + wave * 32 * kOutPieces;
+    static_assert(WAVES * 32 * kOutPieces <= STAGES * kBuffer, "fits the buffers");
+    uintx4* mine = buffers + wave * 32 * kOutPieces;
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
 #pragma unroll
@@ -582,91 +694,126 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN > 128 * 128 ? 1 : 2) pro
 }
 
 // ------------------------------------------------------------------ a few rows
-// Up to 16 MT rows of a group by 16 columns (rows of the weights) a workgroup.  What counts is that the weights come once and at
-// the memory's rate: every wave reads its share of the depth, 64 bytes of a row at a time, straight into the registers that the
-// matrix pipe takes, and the four partial sums meet in LDS.
-template <int TYPE, int MT, typename Out>
+// Up to 16 rows of a group by 16 NT columns (rows of the weights) a workgroup.  What counts is that the weights come once and at
+// the memory's rate: every wave reads its share of the depth, runs of 256 bytes of a row, straight into the registers that the
+// matrix pipe takes, one run ahead, and the four partial sums meet in LDS.
+constexpr int kRunSteps = 4;                              // products of a run, 64 bytes of a row each
+template <int TYPE, int NT>
+struct Run {
+    uintx4 w[NT][kRunSteps], x[kRunSteps];
+    uintx4 ws[NT], xs;                                    // kMx4: the run's scales of the lane's rows
+};
+template <int TYPE, int NT, typename Out>
 __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned columns)
 {
     constexpr bool MX = TYPE == kMx4;
-    __shared__ floatx4 part[4][MT][64];
+    __shared__ floatx4 part[4][NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, quarter = lane >> 4;
-    RowTiles<16 * MT> tiles(p);
+    RowTiles<16> tiles(p);
     unsigned tile;
     if (!xcd_run(blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
     const RowTile at = tiles.find(tile / columns);
-    const int n0 = tile % columns * 16;
+    const int n0 = tile % columns * (16 * NT);
     const bool nobody = at.expert == p.experts;
     const int rows_left = at.hi - at.lo;
     const int bytes = nobody ? 0 : (MX ? p.depth / 2 : p.depth * 2);
-    const int n = n0 + r16 < p.width ? n0 + r16 : p.width - 1;
-    const long long weight_row = (nobody ? 0 : at.expert) * (long long)p.width + n;
-    const char* w = p.b + (nobody ? 0 : at.expert) * p.b_group + n * p.b_stride + quarter * 16;
-    const char* x[MT];
     const int row_scales = p.depth / kMx4Block;
-    const uint8_t *ws = nullptr, *xs[MT];
-    if constexpr (MX) ws = p.b_scales + weight_row * row_scales + quarter;
+    const int row = at.lo + (r16 < rows_left ? r16 : rows_left - 1);
+    const char *x = p.a + row * p.a_stride + quarter * 16, *w[NT];
+    const uint8_t *xs = p.a_scales + (long long)row * row_scales, *ws[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int r = at.lo + (t * 16 + r16 < rows_left ? t * 16 + r16 : rows_left - 1);
-        x[t] = p.a + r * p.a_stride + quarter * 16;
-        if constexpr (MX) xs[t] = p.a_scales + (long long)r * row_scales + quarter;
+    for (int t = 0; t < NT; ++t) {
+        const int n = n0 + t * 16 + r16 < p.width ? n0 + t * 16 + r16 : p.width - 1;
+        w[t] = p.b + (nobody ? 0 : at.expert) * p.b_group + n * p.b_stride + quarter * 16;
+        ws[t] = p.b_scales + ((nobody ? 0 : at.expert) * (long long)p.width + n) * row_scales;
     }
-    floatx4 acc[MT];
+    floatx4 acc[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = floatx4{0, 0, 0, 0};
-    const int steps = (bytes + 63) / 64, whole = bytes / 64;
-    int s = wave;
-    constexpr int AHEAD = MT > 2 ? 4 : 8;          // steps whose loads are in flight together
-    for (; s + 4 * (AHEAD - 1) < whole; s += 4 * AHEAD) {
-        uintx4 fw[AHEAD], fx[AHEAD][MT];
-        unsigned sw[AHEAD], sx[AHEAD][MT];
+    for (int t = 0; t < NT; ++t) acc[t] = floatx4{0, 0, 0, 0};
+
+    const auto piece16 = [](const void* from) {
+        struct __attribute__((packed, aligned(1))) Sixteen { unsigned v[4]; };
+        const Sixteen t = *static_cast<const Sixteen*>(from);
+        return uintx4{t.v[0], t.v[1], t.v[2], t.v[3]};
+    };
+    const auto fetch = [&](Run<TYPE, NT>& run, int k) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int at_step = s + 4 * i;
-            fw[i] = fetch_some(w + at_step * 64, 8);
-            if constexpr (MX) sw[i] = ws[at_step * 4];
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                fx[i][t] = fetch_some(x[t] + at_step * 64, 8);
-                if constexpr (MX) sx[i][t] = xs[t][at_step * 4];
-            }
+            for (int i = 0; i < kRunSteps; ++i) run.w[t][i] = fetch_some(w[t] + (k * kRunSteps + i) * 64, 8);
+            if constexpr (MX) run.ws[t] = piece16(ws[t] + k * kRunSteps * 4);
         }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
+        for (int i = 0; i < kRunSteps; ++i) run.x[i] = fetch_some(x + (k * kRunSteps + i) * 64, 8);
+        if constexpr (MX) run.xs = piece16(xs + k * kRunSteps * 4);
+    };
+    const auto multiply = [&](const Run<TYPE, NT>& run) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                if constexpr (MX) acc[t] = multiply16_scaled(fw[i], fx[i][t], acc[t], sw[i], sx[i][t]);
-                else acc[t] = multiply16<TYPE>(fw[i], fx[i][t], acc[t]);
+        for (int i = 0; i < kRunSteps; ++i)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if constexpr (MX) acc[t] = multiply16_scaled(run.w[t][i], run.x[i], acc[t], run.ws[t][i] >> (8 * quarter), run.xs[i] >> (8 * quarter));
+                else acc[t] = multiply16<TYPE>(run.w[t][i], run.x[i], acc[t]);
             }
+    };
+    const int runs = bytes / (64 * kRunSteps);
+    Run<TYPE, NT> now, next;
+    int k = wave;
+    if (k < runs) fetch(now, k);
+    for (; k + 4 < runs; k += 4) {
+        fetch(next, k + 4);
+        multiply(now);
+        now = next;
     }
-    for (; s < steps; s += 4) {
+    if (k < runs) multiply(now);
+    // what is left is less than a run: a step a wave
+    for (int s = runs * kRunSteps + wave; s * 64 < bytes; s += 4) {
         const int count = (bytes - s * 64 - quarter * 16) >> 1;        // 16-bit numbers, or pairs of codes
-        const uintx4 fw = fetch_some(w + s * 64, count);
-        unsigned sw = 0x7f;
-        if constexpr (MX)
-            if (count > 0) sw = ws[s * 4];
+        const uintx4 fx = fetch_some(x + s * 64, count);
+        const unsigned sx = MX && count > 0 ? xs[s * 4 + quarter] : 0x7f;
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const uintx4 fx = fetch_some(x[t] + s * 64, count);
-            if constexpr (MX) acc[t] = multiply16_scaled(fw, fx, acc[t], sw, count > 0 ? xs[t][s * 4] : 0x7fu);
+        for (int t = 0; t < NT; ++t) {
+            const uintx4 fw = fetch_some(w[t] + s * 64, count);
+            if constexpr (MX) acc[t] = multiply16_scaled(fw, fx, acc[t], count > 0 ? ws[t][s * 4 + quarter] : 0x7fu, sx);
             else acc[t] = multiply16<TYPE>(fw, fx, acc[t]);
         }
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
+    for (int t = 0; t < NT; ++t) part[wave][t][lane] = acc[t];
     __syncthreads();
     // register v of lane l: column 4 (l / 16) + v, row l % 16
     const bool vector = p.out_stride % 4 == 0;
-    for (int t = wave; t < MT; t += 4) {
+    if (wave < NT && r16 < rows_left) {
+        const int t = wave, col = n0 + t * 16 + 4 * quarter;
         const floatx4 sum = (part[0][t][lane] + part[1][t][lane]) + (part[2][t][lane] + part[3][t][lane]);
-        const int r = t * 16 + r16, col = n0 + 4 * quarter;
-        if (r < rows_left) {
-            Out* out = reinterpret_cast<Out*>(p.out) + (at.lo + r) * p.out_stride + col;
-            store_four(out, sum[0], sum[1], sum[2], sum[3], p.width - col, vector);
+        Out* out = reinterpret_cast<Out*>(p.out) + (at.lo + r16) * p.out_stride + col;
+        store_four(out, sum[0], sum[1], sum[2], sum[3], p.width - col, vector);
+    }
+}
+
+// ------------------------------------------------------------------ sums over shares of the depth
+// out = the sum of `splits` partial results of `count` numbers each, four numbers a thread, always in the same order
+template <typename Out>
+__global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ partial, int splits, long long count, Out* __restrict__ out)
+{
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= count) return;
+    const int left = count - i < 4 ? (int)(count - i) : 4;
+    float v[4] = {0, 0, 0, 0};
+    for (int s = 0; s < splits; ++s) {
+        const float* from = partial + s * count + i;
+        if (left == 4) {
+            const Words4 t = *reinterpret_cast<const Words4*>(from);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += __uint_as_float(t.w[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                if (k < left) v[k] += from[k];
         }
     }
+    store_four(out + i, v[0], v[1], v[2], v[3], left, true);
 }
 
 // ------------------------------------------------------------------ launches
@@ -678,25 +825,43 @@ inline long long row_tiles_at_most(const ProductParams& p, int height)
 }
 constexpr long long kMostBlocks = 0xffffff;       // a grid holds fewer than 2^32 threads
 
-template <int DIRECTION, int TYPE, int BM, int BN, int WM, int WN, bool ANY, typename Out>
-hipError_t launch_tiles(const ProductParams& p, hipStream_t s)
+template <int DIRECTION, int TYPE, int BM, int BN, int STAGES, bool ANY, typename Out>
+hipError_t launch_whole_tiles(const ProductParams& p, hipStream_t s)
 {
     const long long columns = (p.width + BN - 1) / BN;
     long long blocks;
     if (DIRECTION == kDw) blocks = (columns * ((p.height + BM - 1) / BM) + 7) / 8 * 8 * p.experts;
     else blocks = (row_tiles_at_most(p, BM) * columns + 7) / 8 * 8;
-    if (blocks > kMostBlocks) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((product_kernel<DIRECTION, TYPE, BM, BN, WM, WN, ANY, Out>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, p);
+    if (blocks * p.splits > kMostBlocks) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((product_kernel<DIRECTION, TYPE, BM, BN, 2, 2, STAGES, ANY, Out>), dim3((unsigned)blocks, p.splits), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 
-template <int TYPE, int MT, typename Out>
+template <int DIRECTION, int TYPE, int BM, int BN, int STAGES, bool ANY, typename Out>
+hipError_t launch_tiles(const ProductParams& p, hipStream_t s)
+{
+    if constexpr (DIRECTION == kDw)
+        if (p.splits > 1) {
+            ProductParams q = p;
+            const long long count = (long long)p.experts * p.height * p.width, blocks = (count + 1023) / 1024;
+            q.out = static_cast<char*>(p.workspace);
+            q.split_stride = count;
+            const hipError_t e = launch_whole_tiles<DIRECTION, TYPE, BM, BN, STAGES, ANY, float>(q, s);
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL(join_kernel<Out>, dim3((unsigned)blocks), dim3(256), 0, s, static_cast<const float*>(p.workspace), p.splits, count,
+                               reinterpret_cast<Out*>(p.out));
+            return hipGetLastError();
+        }
+    return launch_whole_tiles<DIRECTION, TYPE, BM, BN, STAGES, ANY, Out>(p, s);
+}
+
+template <int TYPE, int NT, typename Out>
 hipError_t launch_few_rows(const ProductParams& p, hipStream_t s)
 {
-    const long long columns = (p.width + 15) / 16;
-    const long long blocks = (row_tiles_at_most(p, 16 * MT) * columns + 7) / 8 * 8;
+    const long long columns = (p.width + 16 * NT - 1) / (16 * NT);
+    const long long blocks = (row_tiles_at_most(p, 16) * columns + 7) / 8 * 8;
     if (blocks > kMostBlocks) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((few_rows_kernel<TYPE, MT, Out>), dim3((unsigned)blocks), dim3(256), 0, s, p, (unsigned)columns);
+    hipLaunchKernelGGL((few_rows_kernel<TYPE, NT, Out>), dim3((unsigned)blocks), dim3(256), 0, s, p, (unsigned)columns);
     return hipGetLastError();
 }
 
@@ -715,22 +880,28 @@ bool whole_pieces(const ProductParams& p)
 template <int DIRECTION, int TYPE, typename Out>
 hipError_t launch_product_as(const ProductParams& p, hipStream_t s)
 {
-    if constexpr (DIRECTION == kForward) {
-        const long long rows = (p.rows + p.experts - 1) / p.experts;      // of a group, on average
-        // (the tiles read scales sixteen at a time)
-        const long long scales = p.depth / kMx4Block;
-        if (TYPE == kMx4 && (p.rows * scales < 16 || p.experts * (p.width * scales) < 16)) return launch_few_rows<TYPE, 1, Out>(p, s);
-        if (rows <= 16) return launch_few_rows<TYPE, 1, Out>(p, s);
-        if (rows <= 32) return launch_few_rows<TYPE, 2, Out>(p, s);
-        if (rows <= 64) return launch_few_rows<TYPE, 4, Out>(p, s);
+    if constexpr (DIRECTION == kForward)
+        if (p.tile == kFewRows) {
+            // Weights' rows a workgroup: more of them share the rows of `a`, fewer leave more workgroups.  16 / 32 / 64, in us: 4 bits, 1 row, n = 8192,
+            // k = 8192 8.8 / 9.9 / 13.7; 16 rows, n = 16384, k = 4096 11.9 / 10.2 / 9.8; 64 rows of 32 experts, n = 4096, k = 2048 26.3 / 22.9 / 22.5;
+            // bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7
+            const long long sixteens = (p.width + 15) / 16 * (long long)(p.experts < p.rows ? p.experts : p.rows);
+            if constexpr (TYPE == kMx4)
+                if (sixteens >= 4096) return launch_few_rows<TYPE, 4, Out>(p, s);
+            if (sixteens >= 1024) return launch_few_rows<TYPE, 2, Out>(p, s);
+            return launch_few_rows<TYPE, 1, Out>(p, s);
+        }
+    if constexpr (TYPE != kMx4) {
+        // (the same order of the sums as with whole pieces: each number's in the order of the depth, or a quarter of each chunk a wave)
+        if (!whole_pieces<DIRECTION, TYPE>(p))
+            return p.tile == kTile64 ? launch_tiles<DIRECTION, TYPE, 64, 64, 2, true, Out>(p, s) : launch_tiles<DIRECTION, TYPE, 128, 128, 2, true, Out>(p, s);
+        if (p.tile == kTile128Deep) return launch_tiles<DIRECTION, TYPE, 128, 128, 4, false, Out>(p, s);
     }
-    if constexpr (TYPE != kMx4)
-        if (!whole_pieces<DIRECTION, TYPE>(p)) return launch_tiles<DIRECTION, TYPE, 128, 128, 2, 2, true, Out>(p, s);
-    long long large;
-    if (DIRECTION == kDw) large = (long long)((p.height + 255) / 256) * ((p.width + 255) / 256) * p.experts;
-    else large = (long long)((p.rows + 255) / 256) * ((p.width + 255) / 256);
-    if (large >= 192) return launch_tiles<DIRECTION, TYPE, 256, 256, 2, 2, false, Out>(p, s);
-    return launch_tiles<DIRECTION, TYPE, 128, 128, 2, 2, false, Out>(p, s);
+    switch (p.tile) {
+    case kTile256: return launch_tiles<DIRECTION, TYPE, 256, 256, 2, false, Out>(p, s);
+    case kTile64: return launch_tiles<DIRECTION, TYPE, 64, 64, 4, false, Out>(p, s);
+    default: return launch_tiles<DIRECTION, TYPE, 128, 128, 2, false, Out>(p, s);
+    }
 }
 
 }  // namespace spinner
