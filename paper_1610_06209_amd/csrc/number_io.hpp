@@ -16,7 +16,9 @@ template <> struct Piece<float> {
     struct Raw { Words4 lo, hi; };
     static __device__ __forceinline__ Raw fetch(const float* p)
     {
-        return {reinterpret_cast<const Words4*>(p)[0], reinterpret_cast<const Words4*>(p)[1]};
+        typedef unsigned Four __attribute__((ext_vector_type(4), aligned(4)));
+        const Four a = __builtin_nontemporal_load(reinterpret_cast<const Four*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const Four*>(p) + 1);
+        return {{{a[0], a[1], a[2], a[3]}}, {{b[0], b[1], b[2], b[3]}}};
     }
     static __device__ __forceinline__ void widen(const Raw& r, float* v)
     {
@@ -42,7 +44,12 @@ template <> struct Piece<float> {
 template <typename T> struct Piece16 {
     typedef T Pair __attribute__((ext_vector_type(2)));
     typedef Bytes16 Raw;
-    static __device__ __forceinline__ Raw fetch(const T* p) { return *reinterpret_cast<const Bytes16*>(p); }
+    static __device__ __forceinline__ Raw fetch(const T* p)
+    {
+        typedef unsigned Four __attribute__((ext_vector_type(4), aligned(2)));
+        const Four a = __builtin_nontemporal_load(reinterpret_cast<const Four*>(p));
+        return {{a[0], a[1], a[2], a[3]}};
+    }
     static __device__ __forceinline__ void widen(const Raw& r, float* v)
     {
 #pragma unroll

@@ -1,0 +1,121 @@
+"""The products at sizes that take each form of the kernels (tiles of 256, 128 and 64, four chunks in LDS, sums in shares), whole
+pieces of rows and others, against 64-bit products; and that a layer trained in 16 bits can be served from 4-bit weights.
+
+Tolerances as in test_gpu_grouped.py and test_gpu_mx.py: (depth / 16 + 16) 2^-23 of the sum of magnitudes for 16-bit operands (one more
+addition a share), (k / 64 + 64) 2^-23 for 4-bit ones, and one rounding of the result."""
+import os
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import mx4_oracle as mx
+
+pytestmark = pytest.mark.gpu
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 2.0 ** -140, "bf16": 2.0 ** -133, "f16": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1610_06209_amd import binding
+
+    class G:
+        pass
+
+    g = G()
+    g.torch, g.b, g.dev = torch, binding, torch.device("cuda:0")
+    g.types = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+    return g
+
+
+def say(*a):
+    print("\n[gpu-case]", *a, file=sys.stderr, flush=True)
+
+
+def ragged(rng, rows, experts, spare):
+    ends = np.concatenate((np.sort(rng.integers(0, rows - spare + 1, experts - 1)), [rows - spare]))
+    return ends.astype(np.int64)
+
+
+def check(got, want, size, depth, out):
+    off = (got.double() - want).abs()
+    bound = want.abs() * (1.01 * HALF_STEP[out]) + size * depth + TINY[out]
+    assert bool((off <= bound).all()), float((off / bound).max())
+
+
+SIZES = [(20000, 40, 136, 3), (20000, 136, 40, 1), (2050, 40, 1032, 3), (2050, 1032, 40, 3), (2050, 40, 4104, 3), (2050, 4104, 40, 1), (70, 4104, 264, 3),
+         (70, 4104, 136, 3), (70, 2056, 2056, 3), (2050, 40, 40, 1), (4100, 264, 40, 3), (8200, 1032, 520, 1), (20000, 2056, 136, 3), (600, 520, 1032, 1)]
+
+
+@pytest.mark.parametrize("off", [0, 3])
+@pytest.mark.parametrize("rows,k,n,experts", SIZES)
+def test_sixteen_bits(gpu, rows, k, n, experts, off):
+    k, n = k + off, n + (1 if off else 0)
+    name = "bf16" if (rows + off) % 3 else "f16"
+    say("forms", name, rows, k, n, experts)
+    t, b = gpu.torch, gpu.b
+    gen = t.Generator(device=gpu.dev)
+    gen.manual_seed(rows + k)
+    x, dy, w = (t.randn(s, generator=gen, device=gpu.dev).to(gpu.types[name]) for s in ((rows, k), (rows, n), (experts, n, k)))
+    ends = ragged(np.random.default_rng(rows), rows, experts, 5)
+    e = t.from_numpy(ends).to(gpu.dev)
+    y, dx = b.spinner_grouped_matmul(x, w, e), b.spinner_grouped_matmul_dx(dy, w, e)
+    dws = {out: b.spinner_grouped_matmul_dw(dy, x, e, gpu.types[out]) for out in ("f32", name)}
+    assert not bool(y[ends[-1]:].any()) and not bool(dx[ends[-1]:].any())
+    for i, (lo, hi) in enumerate(mx.bounds(ends, experts, rows)):
+        xe, dye, we = x[lo:hi].double(), dy[lo:hi].double(), w[i].double()
+        check(y[lo:hi], xe @ we.T, xe.abs() @ we.abs().T, (k / 16 + 16) * 2.0 ** -23, name)
+        check(dx[lo:hi], dye @ we, dye.abs() @ we.abs(), (n / 16 + 16) * 2.0 ** -23, name)
+        for out, dw in dws.items():
+            check(dw[i], dye.T @ xe, dye.abs().T @ xe.abs(), ((hi - lo) / 16 + 32) * 2.0 ** -23, out)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k,n,experts", [(70, 8224, 40, 1), (70, 16416, 140, 2), (2050, 64, 4104, 3), (1100, 4128, 2051, 1), (3000, 544, 2300, 4), (90, 8192, 333, 1),
+                                              (200, 7968, 130, 1), (300, 1120, 515, 2)])
+def test_four_bits(gpu, rows, k, n, experts, out):
+    say("forms, 4 bits", out, rows, k, n, experts)
+    t, b = gpu.torch, gpu.b
+    gen = t.Generator(device=gpu.dev)
+    gen.manual_seed(rows + k)
+    codes = lambda r: t.randint(0, 256, (r, k // 2), generator=gen, device=gpu.dev, dtype=t.uint8)          # noqa: E731
+    scales = lambda r: t.randint(112, 124, (r, k // 32), generator=gen, device=gpu.dev, dtype=t.uint8)      # noqa: E731
+    ac, as_, wc, ws = codes(rows), scales(rows), codes(experts * n), scales(experts * n)
+    ends = ragged(np.random.default_rng(rows), rows, experts, 7)
+    y = b.spinner_mx_matmul(ac, as_, wc.view(experts, n, -1), ws.view(experts, n, -1), t.from_numpy(ends).to(gpu.dev), gpu.types[out])
+    a, w = (t.from_numpy(mx.values(c.cpu().numpy(), s.cpu().numpy())).to(gpu.dev) for c, s in ((ac, as_), (wc, ws)))
+    w = w.view(experts, n, k)
+    assert not bool(y[ends[-1]:].any())
+    for i, (lo, hi) in enumerate(mx.bounds(ends, experts, rows)):
+        check(y[lo:hi], a[lo:hi] @ w[i].T, a[lo:hi].abs() @ w[i].abs().T, (k / 64 + 64) * 2.0 ** -23, out)
+
+
+def test_shares_of_a_sum_need_their_workspace(gpu):
+    say("forms, workspace")
+    t, b = gpu.torch, gpu.b
+    rows, n, k = 4100, 40, 264
+    need = b.spinner_grouped_matmul_dw_workspace_bytes(rows, n, k, 1)
+    assert need > 0 and b.spinner_grouped_matmul_dw_workspace_bytes(16, n, k, 1) == 0 and b.spinner_grouped_matmul_dw_workspace_bytes(-1, n, k, 1) == 0
+    dy, x = t.randn((rows, n), device=gpu.dev).bfloat16(), t.randn((rows, k), device=gpu.dev).bfloat16()
+    want = b.spinner_grouped_matmul_dw(dy, x)
+    scratch = t.full((need,), 255, dtype=t.uint8, device=gpu.dev)             # NaN: what is not written shows
+    assert t.equal(b.spinner_grouped_matmul_dw(dy, x, workspace=scratch), want)
+    with pytest.raises(ValueError):
+        b.spinner_grouped_matmul_dw(dy, x, workspace=scratch[:-1])
+    rc = b.lib.spinner_grouped_matmul_dw(dy.data_ptr(), x.data_ptr(), 1, rows, n, k, n, k, 1, None, want.data_ptr(), 0, None, None)
+    assert rc == b.SPINNER_ERR_WORKSPACE
+
+
+def test_example_trains_and_serves(gpu):
+    say("example")
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import expert_layer
+
+    first, last, served, direct = expert_layer.main(rows=2048, n=1024, width=256, experts=8, steps=30, quiet=True)
+    assert last < 0.5 * first                                 # the layer learns
+    assert served < 2 * last and served < direct              # 4 bits with a rotation serve it, better than without
