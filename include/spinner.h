@@ -408,7 +408,8 @@ int spinner_struct_apply_ws(const float *x, int n, long batch, int kind, const v
  * uint8 [rows][k / 32]: 2^(byte - 127), 255 stands for NaN (every number of
  * its 32 then is NaN, and so is every product with them).
  *
- * Element types of tensors of plain numbers; sums are fp32 throughout.
+ * Element types of tensors of plain numbers; sums are fp32 throughout.  Results
+ * never share memory with operands.
  */
 typedef enum { SPINNER_F32 = 0, SPINNER_BF16 = 1, SPINNER_F16 = 2 } spinner_dtype_t;
 
@@ -422,7 +423,7 @@ typedef enum { SPINNER_F32 = 0, SPINNER_BF16 = 1, SPINNER_F16 = 2 } spinner_dtyp
  *
  *   x         in   device [rows][k] of type dtype, rows x_stride elements apart
  *                  (any stride >= 0, so that a row may be repeated)
- *   rows      in   0 <= rows < 2^31
+ *   rows      in   0 <= rows <= 2^31 - 2^16
  *   k         in   a multiple of 32, up to 2^24
  *   diag      in   device fp32 [k], or NULL for D = I
  *   block     in   0, or a power of two in [32, 4096] that divides k

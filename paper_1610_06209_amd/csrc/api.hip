@@ -883,6 +883,7 @@ int spinner_stream_copy(const float* src, float* dst, size_t count, void* stream
 // ------------------------------------------------------------------ 4-bit numbers and grouped products
 static_assert(SPINNER_F32 == spinner::kF32 && SPINNER_BF16 == spinner::kBf16 && SPINNER_F16 == spinner::kF16, "the element types");
 
+constexpr long kMostRows = 0x7fff0000L;          // room for the last tile's rows
 static bool plain_type(int dtype) { return dtype == SPINNER_F32 || dtype == SPINNER_BF16 || dtype == SPINNER_F16; }
 static bool type16(int dtype) { return dtype == SPINNER_BF16 || dtype == SPINNER_F16; }
 static bool side(int n) { return n >= 1 && n <= (1 << 24); }
@@ -900,7 +901,7 @@ static int launched(hipError_t e)
 static int check_quantize(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block)
 {
     if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
-    if (rows < 0 || rows > 0x7fffffffL) return SPINNER_ERR_BAD_BATCH;
+    if (rows < 0 || rows > kMostRows) return SPINNER_ERR_BAD_BATCH;
     if (!mx4_depth(k) || !stride_in(x_stride)) return SPINNER_ERR_BAD_SHAPE;
     if (block && (block < 32 || block > spinner::kMaxRotation || (block & (block - 1)) || k % block)) return SPINNER_ERR_BAD_SHAPE;
     if (diag && !block) return SPINNER_ERR_BAD_SHAPE;
@@ -924,7 +925,7 @@ int spinner_mx_quantize(const void* x, int dtype, long rows, int k, long x_strid
 int spinner_mx_dequantize(const void* codes, const void* scales, long rows, int k, void* out, int dtype, long out_stride, void* stream)
 {
     if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
-    if (rows < 0 || rows > 0x7fffffffL) return SPINNER_ERR_BAD_BATCH;
+    if (rows < 0 || rows > kMostRows) return SPINNER_ERR_BAD_BATCH;
     if (!mx4_depth(k) || !stride_out(out_stride, k, rows)) return SPINNER_ERR_BAD_SHAPE;
     if (rows == 0) return SPINNER_OK;
     if (!codes || !scales || !out) return SPINNER_ERR_NULL_PTR;
@@ -936,7 +937,7 @@ int spinner_mx_dequantize(const void* codes, const void* scales, long rows, int 
 // rows, experts and their ends
 static int check_groups(long rows, int experts, const long long* ends)
 {
-    if (rows < 0 || rows > 0x7fffffffL) return SPINNER_ERR_BAD_BATCH;
+    if (rows < 0 || rows > kMostRows) return SPINNER_ERR_BAD_BATCH;
     if (experts < 1 || experts > spinner::kMaxExperts) return SPINNER_ERR_BAD_SHAPE;
     if (experts > 1 && !ends) return SPINNER_ERR_NULL_PTR;
     if (reinterpret_cast<uintptr_t>(ends) & 7u) return SPINNER_ERR_ALIGNMENT;
@@ -973,7 +974,7 @@ int spinner_mx_matmul(const void* a_codes, const void* a_scales, long rows, int 
 
 size_t spinner_mx_linear_workspace_bytes(long rows, int k)
 {
-    if (rows < 0 || rows > 0x7fffffffL || !mx4_depth(k)) return 0;
+    if (rows < 0 || rows > kMostRows || !mx4_depth(k)) return 0;
     return (size_t)rows * (k / 2 + k / spinner::kMx4Block);
 }
 
@@ -1053,7 +1054,7 @@ static spinner::ProductParams dw_params(long rows, int n, int k, int experts, co
 
 size_t spinner_grouped_matmul_dw_workspace_bytes(long rows, int n, int k, int experts)
 {
-    if (rows < 0 || rows > 0x7fffffffL || experts < 1 || experts > spinner::kMaxExperts || !side(n) || !side(k)) return 0;
+    if (rows < 0 || rows > kMostRows || experts < 1 || experts > spinner::kMaxExperts || !side(n) || !side(k)) return 0;
     return spinner::product_workspace(dw_params(rows, n, k, experts, nullptr));
 }
 
