@@ -176,18 +176,39 @@ __device__ __forceinline__ void store_piece(Out* p, uintx4 v, int left)
     }
 }
 
-// up to eight 16-bit numbers from an address of any alignment, zeros behind them
-__device__ __forceinline__ uintx4 fetch_some(const char* p, int count)
+// Eight 16-bit numbers of a row from an address of any alignment, `count` of them inside the row and zeros behind: a piece that the row's end cuts
+// is read as the eight numbers in front of the end, and one outside (count <= 0) from `safe`; keep_some() then puts it right.  In two
+// halves so that loads in flight are not waited for one by one (number by number, one cut piece a row made 20000 x 301 x 403 weight gradients
+// of 16 experts 298 us).  A row of less than eight numbers (SHORT) is read number by number.
+__device__ __forceinline__ uintx4 fetch_some(const char* p, int count, const char* safe)
 {
-    if (count >= 8) {
-        const Bytes16 t = *reinterpret_cast<const Bytes16*>(p);
-        return uintx4{t.w[0], t.w[1], t.w[2], t.w[3]};
-    }
+    const char* from = count >= 8 ? p : (count > 0 ? p - 2 * (8 - count) : safe);
+    const Bytes16 t = *reinterpret_cast<const Bytes16*>(from);
+    return uintx4{t.w[0], t.w[1], t.w[2], t.w[3]};
+}
+__device__ __forceinline__ uintx4 keep_some(uintx4 v, int count)
+{
+    if (__builtin_expect(__ballot(count < 8) == 0, 1)) return v;
+    unsigned long long lo = v[0] | (unsigned long long)v[1] << 32, hi = v[2] | (unsigned long long)v[3] << 32;
+    const int cut = count >= 8 ? 0 : (count > 0 ? 8 - count : 8), bits = 16 * (cut & 3);
+    if (cut & 4) { lo = hi; hi = 0; }
+    if (cut == 8) { lo = hi = 0; }
+    lo = lo >> bits | (bits ? hi << (64 - bits) : 0);
+    hi >>= bits;
+    return uintx4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+__device__ __forceinline__ uintx4 fetch_short(const char* p, int count)
+{
     uintx4 v = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 7; ++i)
         if (i < count) v[i >> 1] |= (unsigned)reinterpret_cast<const unsigned short*>(p)[i] << (16 * (i & 1));
     return v;
+}
+__device__ __forceinline__ uintx4 fetch_whole(const char* p)
+{
+    const Bytes16 t = *reinterpret_cast<const Bytes16*>(p);
+    return uintx4{t.w[0], t.w[1], t.w[2], t.w[3]};
 }
 
 // ------------------------------------------------------------------ tiles
@@ -253,20 +274,26 @@ struct TileOperand {
         const bool there = DEEP ? load_piece(r, lane) * 16 < depth_left : r < depth_left;
         load_to_lds(lds + (wave * kLoads + T) * 64, from, there ? (unsigned)offset[T] : kFar);
     }
-    // through registers, from any alignment
-    __device__ __forceinline__ void fetch(uintx4 (&v)[kLoads], const char* from, int depth_left, int wave, int lane) const
+    // through registers, from any alignment; `safe`: sixteen bytes that can be read, null for rows of less than eight numbers
+    __device__ __forceinline__ int inside(int t, int depth_left, int wave, int lane) const      // numbers of the t-th piece inside the operand
     {
+        const int r = load_row(t, wave, lane), piece = load_piece(r, lane);
+        return DEEP ? (depth_left - piece * 16) >> 1 : (r < depth_left ? left - piece * 8 : 0);
+    }
+    __device__ __forceinline__ void fetch(uintx4 (&v)[kLoads], const char* from, int depth_left, const char* safe, int wave, int lane) const
+    {
+        if (safe) {
 #pragma unroll
-        for (int t = 0; t < kLoads; ++t) {
-            const int r = load_row(t, wave, lane), piece = load_piece(r, lane);
-            const int count = DEEP ? (depth_left - piece * 16) >> 1 : (r < depth_left ? left - piece * 8 : 0);
-            v[t] = fetch_some(from + offset[t], count);
+            for (int t = 0; t < kLoads; ++t) v[t] = fetch_some(from + offset[t], inside(t, depth_left, wave, lane), safe);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kLoads; ++t) v[t] = fetch_short(from + offset[t], inside(t, depth_left, wave, lane));
         }
     }
-    __device__ __forceinline__ void put(const uintx4 (&v)[kLoads], uintx4* lds, int wave, int lane) const
+    __device__ __forceinline__ void put(const uintx4 (&v)[kLoads], uintx4* lds, int depth_left, const char* safe, int wave, int lane) const
     {
 #pragma unroll
-        for (int t = 0; t < kLoads; ++t) lds[(wave * kLoads + t) * 64 + lane] = v[t];
+        for (int t = 0; t < kLoads; ++t) lds[(wave * kLoads + t) * 64 + lane] = safe ? keep_some(v[t], inside(t, depth_left, wave, lane)) : v[t];
     }
     // operand of the 32 rows from `first` on, step s of four
     static __device__ __forceinline__ uintx4 operand(const uintx4* lds, int first, int s, int lane)
@@ -448,16 +475,20 @@ product_kernel(ProductParams p)
     const int depth_b = DIRECTION == kDx ? depth / 2 : depth;
 
     uintx4 va[ANY ? A::kLoads : 1], vb[ANY ? B::kLoads : 1];
+    // numbers of A's and B's rows as they lie, and the last eight in front of the end of the tile's first
+    const int row_a = DIRECTION == kDw ? p.height : p.depth, row_b = DIRECTION == kForward ? p.depth : p.width;
+    const char* safe_a = ANY && row_a >= 8 && chunks ? (DIRECTION == kDw && rows_left < 8 ? a - 2 * (8 - rows_left) : a) : nullptr;
+    const char* safe_b = ANY && row_b >= 8 && chunks ? (DIRECTION != kForward && cols_left < 8 ? b - 2 * (8 - cols_left) : b) : nullptr;
     const auto fetch = [&](int c) {
         if constexpr (ANY) {
-            oa.fetch(va, a + c * step_a, depth - c * unit_a, wave, lane);
-            ob.fetch(vb, b + c * step_b, depth_b - c * unit_b, wave, lane);
+            oa.fetch(va, a + c * step_a, depth - c * unit_a, safe_a, wave, lane);
+            ob.fetch(vb, b + c * step_b, depth_b - c * unit_b, safe_b, wave, lane);
         }
     };
-    const auto put = [&](uintx4* buffer) {
+    const auto put = [&](int c, uintx4* buffer) {
         if constexpr (ANY) {
-            oa.put(va, buffer, wave, lane);
-            ob.put(vb, buffer + BM * kChunkPieces, wave, lane);
+            oa.put(va, buffer, depth - c * unit_a, safe_a, wave, lane);
+            ob.put(vb, buffer + BM * kChunkPieces, depth_b - c * unit_b, safe_b, wave, lane);
         }
     };
     // Scales (kMx4) of row r of the tile (B's behind A's) from byte `at` of its own on
@@ -489,7 +520,7 @@ product_kernel(ProductParams p)
     int at = 0;                    // buffer of the chunk at hand
     // Chunks behind the last are zeros: they are asked for, and not multiplied but for one that makes 4-bit chunks pairs.
     fetch(0);
-    put(buffers);
+    put(0, buffers);
     fetch(1);
     static_for<0, STAGES - 1>([&](auto k) { static_for<0, kLoads>([&](auto l) { load(l, k.value, buffers + k.value * kBuffer); }); });
     if constexpr (TM * TN > 1) {
@@ -559,7 +590,7 @@ product_kernel(ProductParams p)
             if constexpr (MX && first.value) fetch_scales(c + 2);
             step(s1, now, s2, s0, s0, 0, nullptr);
             step(s2, now, s3, s0, s0, 0, nullptr);
-            put(next);
+            put(c + 1, next);
             meet(behind);
             fetch(c + 2);
             if constexpr (MX && first.value) put_scales(c + 2);
@@ -608,7 +639,7 @@ product_kernel(ProductParams p)
             uintx4* now = buffers + at * kBuffer;
             at = at + 1 < STAGES ? at + 1 : 0;
             uintx4* next = buffers + at * kBuffer;
-            put(next);
+            put(c + 1, next);
             meet(behind);
             if constexpr (MX) {
                 const int shift = (lane >> 5) * 8 + (wave & 1) * 16;
@@ -746,11 +777,11 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int i = 0; i < kRunSteps; ++i) run.w[t][i] = fetch_some(w[t] + (k * kRunSteps + i) * 64, 8);
+            for (int i = 0; i < kRunSteps; ++i) run.w[t][i] = fetch_whole(w[t] + (k * kRunSteps + i) * 64);
             if constexpr (MX) run.ws[t] = piece16(ws[t] + k * kRunSteps * 4);
         }
 #pragma unroll
-        for (int i = 0; i < kRunSteps; ++i) run.x[i] = fetch_some(x + (k * kRunSteps + i) * 64, 8);
+        for (int i = 0; i < kRunSteps; ++i) run.x[i] = fetch_whole(x + (k * kRunSteps + i) * 64);
         if constexpr (MX) run.xs = piece16(xs + k * kRunSteps * 4);
     };
     const auto multiply = [&](const Run<TYPE, NT>& run) {
@@ -773,15 +804,35 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
     }
     if (k < runs) multiply(now);
     // what is left is less than a run: a step a wave
-    for (int s = runs * kRunSteps + wave; s * 64 < bytes; s += 4) {
+    if (const int s = runs * kRunSteps + wave; s * 64 < bytes) {
         const int count = (bytes - s * 64 - quarter * 16) >> 1;        // 16-bit numbers, or pairs of codes
-        const uintx4 fx = fetch_some(x + s * 64, count);
-        const unsigned sx = MX && count > 0 ? xs[s * 4 + quarter] : 0x7f;
+        uintx4 fw[NT], fx;
+        unsigned sw[NT], sx = 0x7f;
+        if (bytes < 16) {
+            fx = fetch_short(x, count);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) fw[t] = fetch_short(w[t], count);
+        } else {
+            // (the first bytes of the row can be read in place of what lies outside)
+            fx = fetch_some(x + s * 64, count, x - quarter * 16);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) fw[t] = fetch_some(w[t] + s * 64, count, w[t] - quarter * 16);
+        }
+        if constexpr (MX) {
+            const int at_scale = s * 4 + (count > 0 ? quarter : 0);
+            sx = count > 0 ? xs[at_scale] : 0x7f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sw[t] = count > 0 ? ws[t][at_scale] : 0x7f;
+        }
+        if (bytes >= 16) {
+            fx = keep_some(fx, count);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) fw[t] = keep_some(fw[t], count);
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const uintx4 fw = fetch_some(w[t] + s * 64, count);
-            if constexpr (MX) acc[t] = multiply16_scaled(fw, fx, acc[t], count > 0 ? ws[t][s * 4 + quarter] : 0x7fu, sx);
-            else acc[t] = multiply16<TYPE>(fw, fx, acc[t]);
+            if constexpr (MX) acc[t] = multiply16_scaled(fw[t], fx, acc[t], sw[t], sx);
+            else acc[t] = multiply16<TYPE>(fw[t], fx, acc[t]);
         }
     }
 #pragma unroll
