@@ -148,7 +148,7 @@ __device__ __forceinline__ void store_four(Out* p, float a, float b, float c, fl
         if constexpr (sizeof(Out) == 4) {
             *reinterpret_cast<floatx4*>(p) = floatx4{a, b, c, d};
         } else {
-            const uint2 t = {Piece<Out>::narrow(a, b), Piece<Out>::narrow(c, d)};
+            const uint2 t = {Pair16<Out>::narrow(a, b), Pair16<Out>::narrow(c, d)};
             *reinterpret_cast<uint2*>(p) = t;
         }
         return;
@@ -714,7 +714,7 @@ product_kernel(ProductParams p)
                 const int r = lane & 31, col = u * 32 + 8 * q + 4 * (lane >> 5), piece = (col / kPieceOuts) ^ (r & (kOutPieces - 1));
                 const float *v = reinterpret_cast<const float*>(&acc[t][u]) + 4 * q;
                 if constexpr (sizeof(Out) == 4) mine[r * kOutPieces + piece] = uintx4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                else reinterpret_cast<uint2*>(mine + r * kOutPieces + piece)[lane >> 5] = uint2{Piece<Out>::narrow(v[0], v[1]), Piece<Out>::narrow(v[2], v[3])};
+                else reinterpret_cast<uint2*>(mine + r * kOutPieces + piece)[lane >> 5] = uint2{Pair16<Out>::narrow(v[0], v[1]), Pair16<Out>::narrow(v[2], v[3])};
             }
 #pragma unroll
         for (int k = 0; k < 32 * kOutPieces / 64; ++k) {
