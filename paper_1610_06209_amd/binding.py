@@ -811,6 +811,7 @@ def spinner_struct_apply_ws(x, kind, spectrum, d1, d2, m=None, scale=1.0, out=No
 
 
 # ------------------------------------------------------------------ 4-bit numbers and products of rows grouped by expert
+_native_products = _native._products
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MX4_BLOCK = 32
 
@@ -904,7 +905,7 @@ def spinner_mx_quantize(x, diag=None, block=0, codes=None, scales=None, stream=N
     x: fp32, bf16 or fp16 CUDA tensor [rows][k], rows any distance apart, k a multiple of 32.  diag: fp32 [k] or None (D = I).
     Returns (codes uint8 [rows][k / 2], scales uint8 [rows][k / 32]); see include/spinner.h for the format.
     """
-    r = _native.mx_quantize(x, diag, block, codes, scales, stream)
+    r = _native_products.mx_quantize(x, diag, block, codes, scales, stream)
     if r is not None:
         return r
     stride = _check_rows(x, "x")
@@ -925,7 +926,7 @@ def spinner_mx_quantize(x, diag=None, block=0, codes=None, scales=None, stream=N
 
 def spinner_mx_dequantize(codes, scales, dtype=torch.float32, out=None, stream=None):
     """The numbers that 4-bit codes stand for: [rows][k] of ``dtype``."""
-    r = _native.mx_dequantize(codes, scales, dtype, out, stream)
+    r = _native_products.mx_dequantize(codes, scales, dtype, out, stream)
     if r is not None:
         return r
     _check_here(codes, "codes", torch.uint8, 2)
@@ -946,7 +947,7 @@ def spinner_mx_matmul(a_codes, a_scales, w_codes, w_scales, ends=None, dtype=tor
     codes and scales as spinner_mx_quantize gives them (w's with the experts in front); ends: int64 CUDA tensor [experts],
     cumulative.  Rows from the last end on come out as 0.
     """
-    r = _native.mx_matmul(a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream)
+    r = _native_products.mx_matmul(a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream)
     if r is not None:
         return r
     _check_here(a_codes, "a_codes", torch.uint8, 2)
@@ -975,7 +976,7 @@ def spinner_mx_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, out=N
 
     The weights are quantised with the same diag and block, which then cancel in the product.
     """
-    r = _native.mx_linear(x, w_codes, w_scales, diag, block, ends, out, workspace, stream)
+    r = _native_products.mx_linear(x, w_codes, w_scales, diag, block, ends, out, workspace, stream)
     if r is not None:
         return r
     x_stride = _check_rows(x, "x")
@@ -1018,13 +1019,13 @@ def spinner_grouped_matmul(x, w, ends=None, out=None, stream=None):
 
     ends: int64 CUDA tensor [experts]; the rows of expert e are ends[e - 1] .. ends[e].  Rows from the last end on come out as 0.
     """
-    r = _native.grouped_matmul(x, w, ends, out, stream)
+    r = _native_products.grouped_matmul(x, w, ends, out, stream)
     return r if r is not None else _grouped(lib.spinner_grouped_matmul, x, w, ends, out, stream, True)
 
 
 def spinner_grouped_matmul_dx(dy, w, ends=None, dx=None, stream=None):
     """Gradient of spinner_grouped_matmul with respect to x: dx = dy w of each expert's rows."""
-    r = _native.grouped_matmul_dx(dy, w, ends, dx, stream)
+    r = _native_products.grouped_matmul_dx(dy, w, ends, dx, stream)
     return r if r is not None else _grouped(lib.spinner_grouped_matmul_dx, dy, w, ends, dx, stream, False)
 
 
@@ -1037,7 +1038,7 @@ def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, wo
 
     dtype: fp32, or the type of dy and x.  Experts without rows get zeros.
     """
-    r = _native.grouped_matmul_dw(dy, x, ends, dtype, dw, workspace, stream)
+    r = _native_products.grouped_matmul_dw(dy, x, ends, dtype, dw, workspace, stream)
     if r is not None:
         return r
     dy_stride, x_stride = _check_rows(dy, "dy"), _check_rows(x, "x", dy.dtype)

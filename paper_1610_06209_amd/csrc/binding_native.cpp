@@ -696,10 +696,22 @@ ENTRY_END
 #define METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(apply_signs), METHOD(apply), METHOD(apply_blocks), METHOD(hash), METHOD(hash_signs), METHOD(sign_codes),
                          METHOD(sign_codes_signs), METHOD(angular_gram), METHOD(layer_forward), METHOD(layer_backward), METHOD(sketch),
-                         METHOD(sketch_gram), METHOD(struct_apply_ws), METHOD(mx_quantize), METHOD(mx_dequantize), METHOD(mx_matmul),
-                         METHOD(mx_linear), METHOD(grouped_matmul), METHOD(grouped_matmul_dx), METHOD(grouped_matmul_dw), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(sketch_gram), METHOD(struct_apply_ws), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+// the calls of the 4-bit and grouped products, in a module of their own inside the first
+PyMethodDef product_methods[] = {METHOD(mx_quantize), METHOD(mx_dequantize), METHOD(mx_matmul), METHOD(mx_linear), METHOD(grouped_matmul),
+                                 METHOD(grouped_matmul_dx), METHOD(grouped_matmul_dw), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef product_module_def = {PyModuleDef_HEAD_INIT, "_native._products", nullptr, -1, product_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__native() { return PyModule_Create(&module_def); }
+PyMODINIT_FUNC PyInit__native()
+{
+    PyObject *module = PyModule_Create(&module_def), *products = module ? PyModule_Create(&product_module_def) : nullptr;
+    if (!products || PyModule_AddObject(module, "_products", products) != 0) {
+        Py_XDECREF(products);
+        Py_XDECREF(module);
+        return nullptr;
+    }
+    return module;
+}

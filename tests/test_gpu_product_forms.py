@@ -119,3 +119,23 @@ def test_example_trains_and_serves(gpu):
     first, last, served, direct = expert_layer.main(rows=2048, n=1024, width=256, experts=8, steps=30, quiet=True)
     assert last < 0.5 * first                                 # the layer learns
     assert served < 2 * last and served < direct              # 4 bits with a rotation serve it, better than without
+
+
+def test_usual_calls_are_served_natively(gpu):
+    """The native part answers the usual calls itself, and hands on what is out of the ordinary (None)."""
+    say("native part of the binding")
+    t, b = gpu.torch, gpu.b
+    native = b._native_products
+    x, d, w = t.randn((6, 128), device=gpu.dev), t.ones(128, device=gpu.dev), t.randn((10, 128), device=gpu.dev)
+    codes, scales = native.mx_quantize(x, d, 64, None, None, None)
+    wc, ws = native.mx_quantize(w, d, 64, None, None, None)
+    h, hw, dy = x.bfloat16(), w.bfloat16(), t.randn((6, 10), device=gpu.dev).bfloat16()
+    served = [native.mx_dequantize(codes, scales, t.float32, None, None), native.mx_matmul(codes, scales, wc, ws, None, t.float16, None, None),
+              native.mx_linear(h, wc, ws, d, 64, None, None, None, None), native.grouped_matmul(h, hw, None, None, None),
+              native.grouped_matmul_dx(dy, hw, None, None, None), native.grouped_matmul_dw(dy, h, None, t.float32, None, None, None)]
+    assert all(r is not None for r in served)
+    side = t.cuda.current_stream()
+    handed_on = [native.mx_quantize(x, d, 64, None, None, side), native.mx_quantize(x[:, :64], None, 0, None, None, None), native.mx_quantize(x.cpu(), None, 0, None, None, None),
+                 native.mx_quantize(x, d, 48, None, None, None), native.mx_linear(x.double(), wc, ws, d, 64, None, None, None, None),
+                 native.grouped_matmul(h, hw.half(), None, None, None), native.grouped_matmul(x, w, None, None, None), native.grouped_matmul(dy, hw, None, None, None)]
+    assert all(r is None for r in handed_on)
