@@ -472,19 +472,29 @@ bool dtype_of(PyObject* o, at::ScalarType* type, int* code)
     *type = reinterpret_cast<THPDtype*>(o)->scalar_type;
     return element_type(*type, code);
 }
-// contiguous rows of plain numbers on the GPU that the call runs on
-const Tensor* number_rows(PyObject* o, long* count, int* width, int* code)
+// a contiguous tensor on the GPU that the call runs on
+const Tensor* here(PyObject* o)
 {
     const Tensor* t = gpu_tensor(o);
+    return t && t->get_device() == c10::hip::current_device() ? t : nullptr;
+}
+const Tensor* here(PyObject* o, at::ScalarType type)
+{
+    const Tensor* t = here(o);
+    return t && t->scalar_type() == type ? t : nullptr;
+}
+// rows of plain numbers
+const Tensor* number_rows(PyObject* o, long* count, int* width, int* code)
+{
+    const Tensor* t = here(o);
     if (!t || t->dim() != 2 || t->size(1) > INT_MAX || !element_type(t->scalar_type(), code)) return nullptr;
-    if (t->get_device() != c10::hip::current_device()) return nullptr;
     *count = (long)t->size(0);
     *width = (int)t->size(1);
     return t;
 }
 const Tensor* byte_rows(PyObject* o, long count, int64_t width)
 {
-    const Tensor* t = typed_tensor(o, at::kByte);
+    const Tensor* t = here(o, at::kByte);
     return t && t->dim() == 2 && t->size(0) == count && t->size(1) == width ? t : nullptr;
 }
 // [n][k] or [experts][n][k]
@@ -500,7 +510,7 @@ bool expert_ends(PyObject* o, int experts, const long long** ends)
 {
     *ends = nullptr;
     if (o == Py_None) return experts == 1;
-    const Tensor* t = typed_tensor(o, at::kLong);
+    const Tensor* t = here(o, at::kLong);
     if (!t || t->dim() != 1 || t->numel() != experts) return false;
     *ends = static_cast<const long long*>(t->data_ptr());
     return true;
@@ -509,7 +519,7 @@ bool result_rows(PyObject* o, const Tensor** given, at::ScalarType type, long co
 {
     *given = nullptr;
     if (o == Py_None) return true;
-    const Tensor* t = typed_tensor(o, type);
+    const Tensor* t = here(o, type);
     if (!t || t->dim() != 2 || t->size(0) != count || t->size(1) != width) return false;
     *given = t;
     return true;
@@ -523,8 +533,8 @@ bool rotation(PyObject* diag, PyObject* block, int k, const Tensor** d, int* b)
     *d = nullptr;
     if (!whole(block, b)) return false;
     if (diag == Py_None) return true;
-    *d = floats(diag, k);
-    return *d && (*d)->dim() == 1;
+    *d = here(diag, at::kFloat);
+    return *d && (*d)->dim() == 1 && (*d)->numel() == k;
 }
 
 // x, diag, block, codes, scales, stream
@@ -554,11 +564,10 @@ ENTRY_END
 
 // codes, scales, dtype, out, stream
 ENTRY(mx_dequantize, 5)
-    const Tensor *codes = typed_tensor(a[0], at::kByte), *given;
+    const Tensor *codes = here(a[0], at::kByte), *given;
     at::ScalarType type;
     int code;
     if (!codes || codes->dim() != 2 || codes->size(1) % 16 || codes->size(1) > INT_MAX / 2 || a[4] != Py_None || !dtype_of(a[2], &type, &code)) LONG_WAY;
-    if (codes->get_device() != c10::hip::current_device()) LONG_WAY;
     const long count = (long)codes->size(0);
     const int k = 2 * (int)codes->size(1);
     const Tensor* scales = byte_rows(a[1], count, k / 32);
@@ -576,13 +585,12 @@ ENTRY_END
 
 // a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream
 ENTRY(mx_matmul, 8)
-    const Tensor *codes = typed_tensor(a[0], at::kByte), *wc = typed_tensor(a[2], at::kByte), *ws = typed_tensor(a[3], at::kByte), *given;
+    const Tensor *codes = here(a[0], at::kByte), *wc = here(a[2], at::kByte), *ws = here(a[3], at::kByte), *given;
     at::ScalarType type;
     int code, experts, n, experts_s, n_s;
     int64_t half, blocks;
     const long long* ends;
     if (!codes || codes->dim() != 2 || codes->size(1) % 16 || codes->size(1) > INT_MAX / 2 || a[7] != Py_None || !dtype_of(a[5], &type, &code)) LONG_WAY;
-    if (codes->get_device() != c10::hip::current_device()) LONG_WAY;
     const long count = (long)codes->size(0);
     const int k = 2 * (int)codes->size(1);
     const Tensor* scales = byte_rows(a[1], count, k / 32);
@@ -606,14 +614,14 @@ ENTRY(mx_linear, 9)
     int k, code, block, experts, n, experts_s, n_s;
     int64_t half, blocks;
     const long long* ends;
-    const Tensor *x = number_rows(a[0], &count, &k, &code), *wc = typed_tensor(a[1], at::kByte), *ws = typed_tensor(a[2], at::kByte), *d, *given;
+    const Tensor *x = number_rows(a[0], &count, &k, &code), *wc = here(a[1], at::kByte), *ws = here(a[2], at::kByte), *d, *given;
     if (!x || a[8] != Py_None || k % 32 || !rotation(a[3], a[4], k, &d, &block)) LONG_WAY;
     if (!weights(wc, &experts, &n, &half) || !weights(ws, &experts_s, &n_s, &blocks) || half != k / 2 || blocks != k / 32) LONG_WAY;
     if (wc->dim() != ws->dim() || experts_s != experts || n_s != n || !expert_ends(a[5], experts, &ends)) LONG_WAY;
     if (!result_rows(a[6], &given, x->scalar_type(), count, n)) LONG_WAY;
     const size_t need = spinner_mx_linear_workspace_bytes(count, k);
     Buffer w;
-    if (!w.usable_bytes(a[7], need)) LONG_WAY;
+    if ((a[7] != Py_None && !here(a[7])) || !w.usable_bytes(a[7], need)) LONG_WAY;
     Tensor out;
     int rc;
     {
@@ -633,7 +641,7 @@ PyObject* grouped(Args a, bool across)
     int depth, code, experts, n;
     int64_t k;
     const long long* ends;
-    const Tensor *x = number_rows(a[0], &count, &depth, &code), *w = gpu_tensor(a[1]), *given;
+    const Tensor *x = number_rows(a[0], &count, &depth, &code), *w = here(a[1]), *given;
     if (!x || a[4] != Py_None || !weights(w, &experts, &n, &k) || k > INT_MAX || w->scalar_type() != x->scalar_type()) LONG_WAY;
     if (depth != (across ? k : n) || !expert_ends(a[2], experts, &ends)) LONG_WAY;
     const int width = across ? n : (int)k;
@@ -667,19 +675,19 @@ ENTRY(grouped_matmul_dw, 7)
     const Tensor *dy = number_rows(a[0], &count, &n, &code), *x = number_rows(a[1], &x_count, &k, &x_code), *given = nullptr;
     if (!dy || !x || a[6] != Py_None || x_count != count || x_code != code || !dtype_of(a[3], &type, &dw_code)) LONG_WAY;
     if (a[2] != Py_None) {
-        const Tensor* e = typed_tensor(a[2], at::kLong);
+        const Tensor* e = here(a[2], at::kLong);
         if (!e || e->dim() != 1 || e->numel() < 1 || e->numel() > INT_MAX) LONG_WAY;
         experts = (int)e->numel();
         ends = static_cast<const long long*>(e->data_ptr());
     }
     const std::vector<int64_t> sizes = ends ? std::vector<int64_t>{experts, n, k} : std::vector<int64_t>{n, k};
     if (a[4] != Py_None) {
-        given = typed_tensor(a[4], type);
+        given = here(a[4], type);
         if (!given || given->sizes() != at::IntArrayRef(sizes)) LONG_WAY;
     }
     const size_t need = spinner_grouped_matmul_dw_workspace_bytes(count, n, k, experts);
     Buffer w;
-    if (!w.usable_bytes(a[5], need)) LONG_WAY;
+    if ((a[5] != Py_None && !here(a[5])) || !w.usable_bytes(a[5], need)) LONG_WAY;
     Tensor dw;
     int rc;
     {
