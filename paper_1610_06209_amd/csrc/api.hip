@@ -944,16 +944,9 @@ static int check_groups(long rows, int experts, const long long* ends)
     return SPINNER_OK;
 }
 
-int spinner_mx_matmul(const void* a_codes, const void* a_scales, long rows, int k, const void* w_codes, const void* w_scales, int n,
-                       int experts, const long long* ends, void* out, int dtype, long out_stride, void* stream)
+static spinner::ProductParams mx_params(const void* a_codes, const void* a_scales, long rows, int k, const void* w_codes, const void* w_scales, int n,
+                                        int experts, const long long* ends, void* out, long out_stride)
 {
-    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
-    const int rc = check_groups(rows, experts, ends);
-    if (rc != SPINNER_OK) return rc;
-    if (!mx4_depth(k) || !side(n) || !stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
-    if (rows == 0) return SPINNER_OK;
-    if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
-    if (!aligned16(a_codes) || !aligned16(w_codes) || !aligned16(out)) return SPINNER_ERR_ALIGNMENT;
     spinner::ProductParams p = {};
     p.a = static_cast<const char*>(a_codes);
     p.b = static_cast<const char*>(w_codes);
@@ -969,6 +962,20 @@ int spinner_mx_matmul(const void* a_codes, const void* a_scales, long rows, int 
     p.width = n;
     p.depth = k;
     spinner::plan_product(spinner::kForward, true, &p);
+    return p;
+}
+
+int spinner_mx_matmul(const void* a_codes, const void* a_scales, long rows, int k, const void* w_codes, const void* w_scales, int n,
+                       int experts, const long long* ends, void* out, int dtype, long out_stride, void* stream)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    const int rc = check_groups(rows, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    if (!mx4_depth(k) || !side(n) || !stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(a_codes) || !aligned16(w_codes) || !aligned16(out)) return SPINNER_ERR_ALIGNMENT;
+    const spinner::ProductParams p = mx_params(a_codes, a_scales, rows, k, w_codes, w_scales, n, experts, ends, out, out_stride);
     return launched(spinner::launch_product_mx4(dtype, p, static_cast<hipStream_t>(stream)));
 }
 
@@ -992,9 +999,14 @@ int spinner_mx_linear(const void* x, int dtype, long rows, int k, long x_stride,
     if (!aligned16(w_codes) || !aligned16(out) || !aligned16(workspace)) return SPINNER_ERR_ALIGNMENT;
     uint8_t* codes = static_cast<uint8_t*>(workspace);
     uint8_t* scales = codes + (size_t)rows * (k / 2);
+    const spinner::ProductParams p = mx_params(codes, scales, rows, k, w_codes, w_scales, n, experts, ends, out, out_stride);
+    if (spinner::quantises_within(p)) {
+        const spinner::RawRows raw = {x, diag, x_stride, block ? 1.0f / sqrtf((float)block) : 0.0f, block ? __builtin_ctz(block) : 0};
+        return launched(spinner::launch_product_raw(dtype, p, raw, static_cast<hipStream_t>(stream)));
+    }
     rc = spinner_mx_quantize(x, dtype, rows, k, x_stride, diag, block, codes, scales, stream);
     if (rc != SPINNER_OK) return rc;
-    return spinner_mx_matmul(codes, scales, rows, k, w_codes, w_scales, n, experts, ends, out, dtype, out_stride, stream);
+    return launched(spinner::launch_product_mx4(dtype, p, static_cast<hipStream_t>(stream)));
 }
 
 // forward and dx: rows of `depth` numbers against w [experts][n][k]

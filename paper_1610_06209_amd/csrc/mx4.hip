@@ -1,34 +1,15 @@
 // Rotation and quantisation to microscaled 4-bit floating point (e2m1 with a shared power of two for each 32 numbers), and back.
 #include <math.h>
 
-#include "mx4.hpp"
-#include "number_io.hpp"
-#include "spinner_kernels.hpp"
+#include "mx4_lane.hpp"
 
 namespace spinner {
 namespace {
 
-constexpr int kPieceNumbers = 8;                         // numbers of a lane
-constexpr int kChunk = 64 * kPieceNumbers;               // numbers of a wave that lie side by side
-constexpr int waves_of_run(int log) { return log > 9 ? 1 << (log - 9) : 1; }
-
-// undoes the trade of lane_swap_stage
-template <int LANE_BIT, int Q, int R>
-__device__ __forceinline__ void swap_back(float (&v)[R])
-{
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-        if (!(j & (1 << Q))) lane_swap<LANE_BIT>(v[j], v[j | (1 << Q)]);
-}
-
 // Rows [rows][k] to codes and scales, v = H D x on each run of 2^LOG coordinates first (LOG = 0: v = x).
-// A lane holds eight numbers: eight neighbours of 16 bits, or four and the four 256 further on in fp32, 16 bytes each (eight fp32 neighbours, whose two
-// loads take every second piece of a line, 16384 x 16384: 254 us; so 214).  Index bits up to 2^8 then are register and lane bits; those above
-// are of the wave in its workgroup.  Butterflies in fp32; lane bits 4 and 5 trade places with register bits 1 and 2 for their stage, and
-// the waves of a run meet in LDS, where each lane sums up the 2^(LOG - 9) numbers of its place with their signs (in registers alone, 64
-// numbers a lane at 2^12, a wave's 240 registers left one wave a SIMD: one row of 4096 12.9 us, here 3.5).  The transform's 1 / sqrt(2^LOG) goes into
-// the diagonal.  A scale is shared by four (fp32: eight) neighbouring lanes: the largest magnitude as a whole number (so that a NaN is larger
-// than an infinity and both larger than any number) gives the exponent.
+// Eight numbers a lane (fp32: four and four, 16 bytes each; eight neighbours, whose two loads take every second piece of a line, 16384 x 16384 254 us;
+// so 214).  Waves of a run longer than a wave's 512 numbers meet in LDS (in registers alone, 64 numbers a lane at 2^12, a wave's 240 registers
+// left one wave a SIMD: one row of 4096 12.9 us, here 3.5).
 // A wave stays with its columns, whose diagonal it keeps, and goes down the rows, the next row's numbers asked for ahead.
 // Measured, bf16 16384 x 8192 (340 MB): no rotation 58 us, 5.9 TB/s (the copy rate is 6.2), runs of 512 82 us (bound by the vector ALU: 15 instructions
 // a number), 1024 90, 4096 112 (the sums in LDS).
@@ -36,130 +17,42 @@ template <typename T, int LOG>
 __global__ void __launch_bounds__(LOG > 9 ? 64 * waves_of_run(LOG) : 256) mx4_quantize_kernel(QuantizeParams p, int column_groups, int row_step)
 {
     constexpr int WAVES = waves_of_run(LOG);
-    constexpr int N = kPieceNumbers, HALVES = sizeof(T) == 4 ? 2 : 1, LOW = HALVES == 2 ? 2 : 3;      // index bit of lane bit 0
+    using Lane = LaneNumbers<T>;
     __shared__ float4 meeting[WAVES > 1 ? 2 : 1][WAVES > 1 ? WAVES * 128 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = WAVES > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
     const int group = unit % column_groups;
     int row = unit / column_groups;
     if (row >= row_step) return;
-    // columns of the lane's numbers, 16 bytes of them each; what is not live (a whole run of coordinates is or is not) is read from the row's first
-    const int first = (WAVES > 1 ? group * WAVES + wave : group) * kChunk + (lane << LOW);
-    int safe[HALVES];
-#pragma unroll
-    for (int h = 0; h < HALVES; ++h) safe[h] = first + h * 256 < p.k ? first + h * 256 : 0;
-    // which lanes' numbers a transform leaves negated (see lane_stage_fmac_dpp): a product of those of lane bits 0, 1 and 3 that it has
-    constexpr int negating = (LOG > LOW) | (LOG > LOW + 1) << 1 | (LOG > LOW + 3) << 3;
-    const unsigned flip = __popc(lane & negating) & 1 ? 0x88888888u : 0u;
-    float d[N];
-    if constexpr (LOG > 0) {
-        const float norm = 1.0f / __builtin_sqrtf((float)(1 << LOG));
-        if (p.diag) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float4 a = *reinterpret_cast<const float4*>(p.diag + (HALVES == 2 ? safe[h % HALVES] : safe[0] + 4 * h));
-                d[4 * h] = a.x * norm; d[4 * h + 1] = a.y * norm; d[4 * h + 2] = a.z * norm; d[4 * h + 3] = a.w * norm;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) d[i] = norm;
-        }
-    }
+    const Lane at_lane(WAVES > 1 ? group * WAVES + wave : group, lane, p.k);
+    const unsigned flip = LOG > 0 ? Lane::flip(LOG, lane) : 0;
+    float d[kPieceNumbers];
+    if constexpr (LOG > 0) at_lane.diagonal(d, p.diag, 1.0f / __builtin_sqrtf((float)(1 << LOG)));
     const T* x = static_cast<const T*>(p.x);
-    Quad raw[HALVES];
-    const auto fetch = [&](int r) {
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) raw[h] = stream_quad(x + r * p.x_stride + safe[h]);
-    };
-    fetch(row);
+    Quad raw[Lane::HALVES];
+    at_lane.fetch(raw, x + row * p.x_stride);
     for (int turn = 0; row < p.rows; ++turn) {
-        float v[N];
+        float v[kPieceNumbers];
         widen_quads<T>(raw, v);
         const int at = row;
         row += row_step;
-        if (row < p.rows) fetch(row);
-        if constexpr (LOG > 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] *= d[i];
-            static_for<0, LOW>([&](auto q) { reg_stage<q.value>(v); });
-            if constexpr (HALVES == 2 && LOG > 8) reg_stage<2>(v);
-            // (lane bits 0, 1 and 3 in one instruction a number, which leaves the upper lane's difference negated)
-            static_for<0, 4>([&](auto b) {
-                if constexpr (LOG > LOW + b.value) {
-                    const float coef = (lane >> b.value) & 1 ? -1.0f : 1.0f;
-                    if constexpr (b.value == 2) lane_stage<2>(v, coef);
-                    else lane_stage_fmac_dpp<b.value>(v, coef);
-                }
-            });
-            if constexpr (LOG > LOW + 4) { lane_swap_stage<4, 1>(v); swap_back<4, 1>(v); }
-            if constexpr (LOG > LOW + 5) { lane_swap_stage<5, 2>(v); swap_back<5, 2>(v); }
-        }
+        if (row < p.rows) at_lane.fetch(raw, x + row * p.x_stride);
+        if constexpr (LOG > 0) Lane::within(v, d, LOG, lane);
         if constexpr (WAVES > 1) {
             float4* m = meeting[turn & 1];           // the other one may still be read
-            m[wave * 128 + lane] = make_float4(v[0], v[1], v[2], v[3]);
-            m[wave * 128 + 64 + lane] = make_float4(v[4], v[5], v[6], v[7]);
+            Lane::meet(v, m + wave * 128, lane);
             __syncthreads();
-            float t[N];
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float4 a = m[w * 128 + lane], b = m[w * 128 + 64 + lane];
-                const float sign = __popc(w & wave) & 1 ? -1.0f : 1.0f;
-                const float u[N] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int i = 0; i < N; ++i) t[i] = w == 0 ? u[i] : __builtin_fmaf(u[i], sign, t[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = t[i];
+            Lane::join(v, m, WAVES, wave, lane);
         }
-        unsigned code[HALVES];
-        int byte[HALVES];
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-            constexpr int M = N / HALVES;
-            const float* u = v + h * M;
-            // the largest magnitude, numbers taken as they lie: positive ones in the order of signed whole numbers, negative ones above them in
-            // that of unsigned ones
-            int above = __float_as_int(u[0]);
-            unsigned below = __float_as_uint(u[0]);
-#pragma unroll
-            for (int i = 1; i < M; ++i) {
-                const int a = __float_as_int(u[i]);
-                above = a > above ? a : above;
-                below = (unsigned)a > below ? (unsigned)a : below;
-            }
-            int top = (int)(below & 0x7fffffffu);
-            top = above > top ? above : top;
-            static_for<0, 5 - LOW>([&](auto b) {
-                const int other = lane_xor_i<1 << b.value>(top);
-                top = other > top ? other : top;
-            });
-            const int e = top >> 23;                                     // largest magnitude: 2^(e - 127) and more
-            byte[h] = e == 255 ? 255 : (e > 2 ? e - 2 : 0);
-            const float scale = exponent_value(byte[h]);
-            unsigned c = 0;
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, u[0], u[1], scale, 0);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, u[2], u[3], scale, 1);
-            if constexpr (HALVES == 1) {
-                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, u[4], u[5], scale, 2);
-                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, u[6], u[7], scale, 3);
-            }
-            if constexpr (LOG > 0) c ^= flip;
-            code[h] = e == 255 ? 0 : c;
-        }
-        // eight codes a lane side by side: fp32 lanes come by theirs in pairs, the even one of the first half
-        const bool odd = HALVES == 2 && (lane & 1);
-        int col = first;
-        if constexpr (HALVES == 2) {
-            const unsigned own = (odd ? code[HALVES - 1] : code[0]) & 0xffff, got = lane_xor_i<1>(odd ? code[0] : code[HALVES - 1]) & 0xffff;
-            code[0] = odd ? got | own << 16 : own | got << 16;
-            col = odd ? first - 4 + 256 : first;
-        }
+        unsigned codes;
+        int byte[Lane::HALVES];
+        const int col = at_lane.encode(v, flip, lane, &codes, byte);
         const long long place = (long long)at * p.k;
-        if (col < p.k) *reinterpret_cast<unsigned*>(p.codes + ((place + col) >> 1)) = code[0];
-        if ((lane & ((32 >> LOW) - 1)) == 0)
+        if (col < p.k) *reinterpret_cast<unsigned*>(p.codes + ((place + col) >> 1)) = codes;
+        if ((lane & ((32 >> Lane::LOW) - 1)) == 0)
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h)
-                if (first + h * 256 < p.k) p.scales[(place + first + h * 256) >> 5] = (uint8_t)byte[h];
+            for (int h = 0; h < Lane::HALVES; ++h)
+                if (at_lane.first + h * 256 < p.k) p.scales[(place + at_lane.first + h * 256) >> 5] = (uint8_t)byte[h];
     }
 }
 
@@ -301,6 +194,12 @@ void plan_product(int direction, bool mx4, ProductParams* p)
     }
     if (mx4) shortest(kForms4, direction, true, p);
     else shortest(kForms16, direction, false, p);
+}
+
+bool quantises_within(const ProductParams& p)
+{
+    const int rows = p.rows < 16 ? p.rows : 16;
+    return p.tile == kFewRows && rows * (long long)((p.depth + kChunk - 1) / kChunk) <= kRawChunks;
 }
 
 hipError_t launch_mx4_quantize(const QuantizeParams& p, int dtype, int block, hipStream_t s)

@@ -59,6 +59,19 @@ inline size_t product_workspace(const ProductParams& p)      // bytes of partial
     return p.splits > 1 ? (size_t)p.splits * p.experts * p.height * p.width * sizeof(float) : 0;
 }
 
+// Rows that the product's kernel quantises for itself.
+struct RawRows {
+    const void* x;                        // of the result's type
+    const float* diag;
+    long long stride;                     // elements
+    float norm;                           // 1 / sqrt(2^log)
+    int log;                              // runs of 2^log coordinates; 0: no rotation
+};
+constexpr int kRawChunks = 8;             // chunks of 512 numbers that a workgroup's eight waves quantise, one each
+// whether a group's rows are so few that every workgroup of the product does
+bool quantises_within(const ProductParams& p);
+hipError_t launch_product_raw(int type, const ProductParams& p, const RawRows& raw, hipStream_t s);
+
 hipError_t launch_product_mx4(int out_type, const ProductParams& p, hipStream_t s);           // kForward
 hipError_t launch_product_bf16(int direction, int out_type, const ProductParams& p, hipStream_t s);
 hipError_t launch_product_f16(int direction, int out_type, const ProductParams& p, hipStream_t s);

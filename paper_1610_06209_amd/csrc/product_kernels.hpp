@@ -4,9 +4,7 @@
 // (v_mfma_f32_32x32x16) or 64 of 4 bits (v_mfma_scale_f32_32x32x64, e2m1 with an e8m0 scale for each 32), 16 bytes a lane from
 // either operand.  So one kernel moves bytes for all types, and what differs is the instruction and the scales.
 #pragma once
-#include "mx4.hpp"
-#include "number_io.hpp"
-#include "spinner_kernels.hpp"
+#include "mx4_lane.hpp"
 
 namespace spinner {
 
@@ -739,28 +737,39 @@ struct Run {
     uintx4 w[NT][kRunSteps], x[kRunSteps];
     uintx4 ws[NT], xs;                                    // kMx4: the run's scales of the lane's rows
 };
-template <int TYPE, int NT, typename Out>
-__global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned columns)
+// RAW (4 bits): the rows are plain numbers of type Out.  Every workgroup rotates and quantises them for itself, a chunk of 512 a wave, into LDS, while its
+// first weights are on their way: no launch and no trip through memory in front of them.  The sums are those of two calls, in the same order.  In us, one
+// launch / two: one row, n = 16384, k = 4096, runs of 4096 10.9 / 12.8; n = 4096, k = 2048 5.4 / 5.9; four rows, n = k = 1024 4.3 / 5.2; one row,
+// n = k = 256 3.2 / 4.6.  With four waves that take two chunks each 13.2, four each (two rows) 17.7.
+// (two waves a SIMD: 260 registers, which leave one, 64 rows of 32 experts 43 us for 35)
+template <int TYPE, int NT, typename Out, bool RAW>
+__global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductParams p, unsigned columns, RawRows raw)
 {
     constexpr bool MX = TYPE == kMx4;
-    __shared__ floatx4 part[4][NT][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert(MX || !RAW, "rows are quantised for 4-bit weights");
+    __shared__ float4 meeting[RAW ? kRawChunks * 128 : 1];
+    __shared__ uintx4 own_codes[RAW ? kRawChunks * 16 : 1], own_scales[RAW ? kRawChunks : 1];
+    // waves share the depth by four; RAW: and the columns by two, so that eight waves quantise
+    constexpr int PARTS = RAW ? 2 : 1;
+    __shared__ floatx4 part[4 * PARTS][NT][64];
+    const int lane = threadIdx.x & 63, in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group & 3;
     const int r16 = lane & 15, quarter = lane >> 4;
     RowTiles<16> tiles(p);
     unsigned tile;
     if (!xcd_run(blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
     const RowTile at = tiles.find(tile / columns);
-    const int n0 = tile % columns * (16 * NT);
+    const int n0 = tile % columns * (16 * NT * PARTS);
     const bool nobody = at.expert == p.experts;
     const int rows_left = at.hi - at.lo;
     const int bytes = nobody ? 0 : (MX ? p.depth / 2 : p.depth * 2);
     const int row_scales = p.depth / kMx4Block;
     const int row = at.lo + (r16 < rows_left ? r16 : rows_left - 1);
-    const char *x = p.a + row * p.a_stride + quarter * 16, *w[NT];
-    const uint8_t *xs = MX ? p.a_scales + (long long)row * row_scales : nullptr, *ws[NT];
+    const int row_chunks = (p.depth + kChunk - 1) / kChunk;           // RAW: a row in LDS is so many whole chunks
+    const char *x = RAW ? reinterpret_cast<const char*>(own_codes) + (row - at.lo) * row_chunks * 256 + quarter * 16 : p.a + row * p.a_stride + quarter * 16, *w[NT];
+    const uint8_t *xs = !MX ? nullptr : RAW ? reinterpret_cast<const uint8_t*>(own_scales) + (row - at.lo) * row_chunks * 16 : p.a_scales + (long long)row * row_scales, *ws[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int n = n0 + t * 16 + r16 < p.width ? n0 + t * 16 + r16 : p.width - 1;
+        const int own = n0 + ((in_group >> 2) * NT + t) * 16 + r16, n = own < p.width ? own : p.width - 1;
         w[t] = p.b + (nobody ? 0 : at.expert) * p.b_group + n * p.b_stride + quarter * 16;
         ws[t] = MX ? p.b_scales + ((nobody ? 0 : at.expert) * (long long)p.width + n) * row_scales : nullptr;
     }
@@ -773,6 +782,13 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
         const Sixteen t = *static_cast<const Sixteen*>(from);
         return uintx4{t.v[0], t.v[1], t.v[2], t.v[3]};
     };
+    // the rows' part of a run (RAW: in LDS, where rows and their scales start at whole 16 bytes)
+    const auto take = [&](Run<TYPE, NT>& run, int k) {
+#pragma unroll
+        for (int i = 0; i < kRunSteps; ++i) run.x[i] = RAW ? *reinterpret_cast<const uintx4*>(x + (k * kRunSteps + i) * 64) : fetch_whole(x + (k * kRunSteps + i) * 64);
+        if constexpr (RAW) run.xs = *reinterpret_cast<const uintx4*>(xs + k * kRunSteps * 4);
+        else if constexpr (MX) run.xs = piece16(xs + k * kRunSteps * 4);
+    };
     const auto fetch = [&](Run<TYPE, NT>& run, int k) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -780,11 +796,10 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
             for (int i = 0; i < kRunSteps; ++i) run.w[t][i] = fetch_whole(w[t] + (k * kRunSteps + i) * 64);
             if constexpr (MX) run.ws[t] = piece16(ws[t] + k * kRunSteps * 4);
         }
-#pragma unroll
-        for (int i = 0; i < kRunSteps; ++i) run.x[i] = fetch_whole(x + (k * kRunSteps + i) * 64);
-        if constexpr (MX) run.xs = piece16(xs + k * kRunSteps * 4);
+        if constexpr (!RAW) take(run, k);
     };
-    const auto multiply = [&](const Run<TYPE, NT>& run) {
+    const auto multiply = [&](Run<TYPE, NT>& run, int k) {
+        if constexpr (RAW) take(run, k);
 #pragma unroll
         for (int i = 0; i < kRunSteps; ++i)
 #pragma unroll
@@ -796,25 +811,63 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
     const int runs = bytes / (64 * kRunSteps);
     Run<TYPE, NT> now, next;
     int k = wave;
-    if (k < runs) fetch(now, k);
+    if constexpr (RAW) {
+        // a chunk of a row a wave: the rows asked for first, then the weights
+        using Lane = LaneNumbers<Out>;
+        const int chunks = nobody ? 0 : (rows_left < 16 ? rows_left : 16) * row_chunks, c = in_group, r = c / row_chunks, in_row = c - r * row_chunks;
+        const unsigned flip = raw.log > 0 ? Lane::flip(raw.log, lane) : 0;
+        const Lane l(in_row, lane, p.depth);
+        Quad quads[Lane::HALVES];
+        float d[kPieceNumbers], v[kPieceNumbers];
+        if (c < chunks) {
+            l.fetch(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride);
+            if (raw.log > 0) l.diagonal(d, raw.diag, raw.norm);
+        }
+        if (k < runs) fetch(now, k);
+        if (c < chunks) {
+            widen_quads<Out>(quads, v);
+            if (raw.log > 0) Lane::within(v, d, raw.log, lane);
+            if (raw.log > 9) Lane::meet(v, meeting + c * 128, lane);
+        }
+        if (raw.log > 9) __syncthreads();
+        if (c < chunks) {
+            if (raw.log > 9) {
+                const int own = in_row & (waves_of_run(raw.log) - 1);
+                Lane::join(v, meeting + (c - own) * 128, waves_of_run(raw.log), own, lane);
+            }
+            unsigned codes;
+            int byte[Lane::HALVES];
+            const int col = l.encode(v, flip, lane, &codes, byte), start = in_row * kChunk;
+            // (behind the row's end: zeros)
+            reinterpret_cast<unsigned*>(own_codes)[c * 64 + (col - start) / 8] = col < p.depth ? codes : 0;
+            if ((lane & ((32 >> Lane::LOW) - 1)) == 0)
+#pragma unroll
+                for (int h = 0; h < Lane::HALVES; ++h)
+                    reinterpret_cast<uint8_t*>(own_scales)[c * 16 + (l.first - start + h * 256) / 32] = l.first + h * 256 < p.depth ? byte[h] : 0x7f;
+        }
+        __syncthreads();
+    } else {
+        if (k < runs) fetch(now, k);
+    }
     for (; k + 4 < runs; k += 4) {
         fetch(next, k + 4);
-        multiply(now);
+        multiply(now, k);
         now = next;
     }
-    if (k < runs) multiply(now);
+    if (k < runs) multiply(now, k);
     // what is left is less than a run: a step a wave
     if (const int s = runs * kRunSteps + wave; s * 64 < bytes) {
         const int count = (bytes - s * 64 - quarter * 16) >> 1;        // 16-bit numbers, or pairs of codes
         uintx4 fw[NT], fx;
         unsigned sw[NT], sx = 0x7f;
-        if (bytes < 16) {
+        if (!MX && bytes < 16) {
             fx = fetch_short(x, count);
 #pragma unroll
             for (int t = 0; t < NT; ++t) fw[t] = fetch_short(w[t], count);
         } else {
             // (the first bytes of the row can be read in place of what lies outside)
-            fx = fetch_some(x + s * 64, count, x - quarter * 16);
+            if constexpr (RAW) fx = *reinterpret_cast<const uintx4*>(x + s * 64);
+            else fx = fetch_some(x + s * 64, count, x - quarter * 16);
 #pragma unroll
             for (int t = 0; t < NT; ++t) fw[t] = fetch_some(w[t] + s * 64, count, w[t] - quarter * 16);
         }
@@ -824,7 +877,7 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
 #pragma unroll
             for (int t = 0; t < NT; ++t) sw[t] = count > 0 ? ws[t][at_scale] : 0x7f;
         }
-        if (bytes >= 16) {
+        if (MX || bytes >= 16) {
             fx = keep_some(fx, count);
 #pragma unroll
             for (int t = 0; t < NT; ++t) fw[t] = keep_some(fw[t], count);
@@ -836,13 +889,13 @@ __global__ void __launch_bounds__(256) few_rows_kernel(ProductParams p, unsigned
         }
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) part[wave][t][lane] = acc[t];
+    for (int t = 0; t < NT; ++t) part[in_group][t][lane] = acc[t];
     __syncthreads();
     // register v of lane l: column 4 (l / 16) + v, row l % 16
     const bool vector = p.out_stride % 4 == 0;
-    if (wave < NT && r16 < rows_left) {
-        const int t = wave, col = n0 + t * 16 + 4 * quarter;
-        const floatx4 sum = (part[0][t][lane] + part[1][t][lane]) + (part[2][t][lane] + part[3][t][lane]);
+    if (in_group < NT * PARTS && r16 < rows_left) {
+        const int first = in_group / NT * 4, t = in_group % NT, col = n0 + in_group * 16 + 4 * quarter;
+        const floatx4 sum = (part[first][t][lane] + part[first + 1][t][lane]) + (part[first + 2][t][lane] + part[first + 3][t][lane]);
         Out* out = reinterpret_cast<Out*>(p.out) + (at.lo + r16) * p.out_stride + col;
         store_four(out, sum[0], sum[1], sum[2], sum[3], p.width - col, vector);
     }
@@ -911,13 +964,14 @@ hipError_t launch_tiles(const ProductParams& p, hipStream_t s)
     return launch_whole_tiles<DIRECTION, TYPE, BM, BN, STAGES, ANY, Out>(p, s);
 }
 
-template <int TYPE, int NT, typename Out>
-hipError_t launch_few_rows(const ProductParams& p, hipStream_t s)
+template <int TYPE, int NT, typename Out, bool RAW>
+hipError_t launch_few_rows(const ProductParams& p, const RawRows& raw, hipStream_t s)
 {
-    const long long columns = (p.width + 16 * NT - 1) / (16 * NT);
+    constexpr int width = 16 * NT * (RAW ? 2 : 1);
+    const long long columns = (p.width + width - 1) / width;
     const long long blocks = (row_tiles_at_most(p, 16) * columns + 7) / 8 * 8;
     if (blocks > kMostBlocks) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((few_rows_kernel<TYPE, NT, Out>), dim3((unsigned)blocks), dim3(256), 0, s, p, (unsigned)columns);
+    hipLaunchKernelGGL((few_rows_kernel<TYPE, NT, Out, RAW>), dim3((unsigned)blocks), dim3(RAW ? 512 : 256), 0, s, p, (unsigned)columns, raw);
     return hipGetLastError();
 }
 
@@ -933,20 +987,29 @@ bool whole_pieces(const ProductParams& p)
     return a_row % 8 == 0 && b_row % 8 == 0 && p.a_stride % 16 == 0 && p.b_stride % 16 == 0 && p.b_group % 16 == 0;
 }
 
+// Weights' rows a workgroup: more of them share the rows of `a`, fewer leave more workgroups.  16 / 32 / 64, in us: 4 bits, 1 row, n = 8192,
+// k = 8192 8.8 / 9.9 / 13.7; 16 rows, n = 16384, k = 4096 11.9 / 10.2 / 9.8; 64 rows of 32 experts, n = 4096, k = 2048 26.3 / 22.9 / 22.5;
+// bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7
+template <int TYPE, typename Out, bool RAW>
+hipError_t launch_few_rows_as(const ProductParams& p, const RawRows& raw, hipStream_t s)
+{
+    const long long sixteens = (p.width + 15) / 16 * (long long)(p.experts < p.rows ? p.experts : p.rows);
+    if constexpr (RAW) {              // (columns for two groups of waves)
+        if (sixteens >= 4096) return launch_few_rows<TYPE, 2, Out, true>(p, raw, s);
+        return launch_few_rows<TYPE, 1, Out, true>(p, raw, s);
+    } else {
+        if constexpr (TYPE == kMx4)
+            if (sixteens >= 4096) return launch_few_rows<TYPE, 4, Out, false>(p, raw, s);
+        if (sixteens >= 1024) return launch_few_rows<TYPE, 2, Out, false>(p, raw, s);
+        return launch_few_rows<TYPE, 1, Out, false>(p, raw, s);
+    }
+}
+
 template <int DIRECTION, int TYPE, typename Out>
 hipError_t launch_product_as(const ProductParams& p, hipStream_t s)
 {
     if constexpr (DIRECTION == kForward)
-        if (p.tile == kFewRows) {
-            // Weights' rows a workgroup: more of them share the rows of `a`, fewer leave more workgroups.  16 / 32 / 64, in us: 4 bits, 1 row, n = 8192,
-            // k = 8192 8.8 / 9.9 / 13.7; 16 rows, n = 16384, k = 4096 11.9 / 10.2 / 9.8; 64 rows of 32 experts, n = 4096, k = 2048 26.3 / 22.9 / 22.5;
-            // bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7
-            const long long sixteens = (p.width + 15) / 16 * (long long)(p.experts < p.rows ? p.experts : p.rows);
-            if constexpr (TYPE == kMx4)
-                if (sixteens >= 4096) return launch_few_rows<TYPE, 4, Out>(p, s);
-            if (sixteens >= 1024) return launch_few_rows<TYPE, 2, Out>(p, s);
-            return launch_few_rows<TYPE, 1, Out>(p, s);
-        }
+        if (p.tile == kFewRows) return launch_few_rows_as<TYPE, Out, false>(p, RawRows{}, s);
     if constexpr (TYPE != kMx4) {
         // (the same order of the sums as with whole pieces: each number's in the order of the depth, or a quarter of each chunk a wave)
         if (!whole_pieces<DIRECTION, TYPE>(p))

@@ -12,4 +12,13 @@ hipError_t launch_product_mx4(int out_type, const ProductParams& p, hipStream_t 
     }
 }
 
+hipError_t launch_product_raw(int type, const ProductParams& p, const RawRows& raw, hipStream_t s)
+{
+    switch (type) {
+    case kF32: return launch_few_rows_as<kMx4, float, true>(p, raw, s);
+    case kBf16: return launch_few_rows_as<kMx4, __bf16, true>(p, raw, s);
+    default: return launch_few_rows_as<kMx4, _Float16, true>(p, raw, s);
+    }
+}
+
 }  // namespace spinner

@@ -139,3 +139,39 @@ def test_usual_calls_are_served_natively(gpu):
                  native.mx_quantize(x, d, 48, None, None, None), native.mx_linear(x.double(), wc, ws, d, 64, None, None, None, None),
                  native.grouped_matmul(h, hw.half(), None, None, None), native.grouped_matmul(x, w, None, None, None), native.grouped_matmul(dy, hw, None, None, None)]
     assert all(r is None for r in handed_on)
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,k,n,block,experts", [(1, 32, 1, 32, 1), (1, 32, 17, 0, 1), (1, 480, 33, 32, 1), (1, 544, 31, 0, 1), (1, 1536, 70, 512, 1), (1, 2048, 4100, 1024, 1), (1, 4096, 65, 2048, 1),
+                                                    (1, 4096, 129, 4096, 1), (1, 3840, 48, 256, 1), (1, 4128, 48, 32, 1), (2, 2048, 100, 2048, 1), (2, 1984, 40, 64, 1), (3, 1024, 200, 512, 1),
+                                                    (4, 1024, 31, 1024, 1), (8, 512, 64, 128, 1), (8, 96, 64, 0, 1), (9, 512, 64, 512, 1), (2, 1024, 40, 1024, 5), (5, 480, 50, 32, 3), (1, 2048, 33, 1024, 64)])
+def test_layers_of_few_rows_are_quantise_then_product(gpu, name, rows, k, n, block, experts):
+    """A row or a few through a layer, where the product's workgroups quantise for themselves (sizes on both sides of that): the same bits as in two calls."""
+    say("few rows in one launch", name, rows, k, n, block, experts)
+    t, rng = gpu.torch, np.random.default_rng(rows + k + n)
+    x = t.from_numpy((rng.standard_normal((rows, k)) * np.where(rng.random(k) < 0.05, 20.0, 1.0)).astype(np.float32)).to(gpu.dev).to(gpu.types[name])
+    if rows > 1:
+        x[1, k // 2] = float("nan")          # its 32, or its run; all of its row's results
+    d = t.from_numpy(rng.standard_normal(k).astype(np.float32)).to(gpu.dev) if block else None
+    wc, ws = gpu.b.spinner_mx_quantize(t.from_numpy(rng.standard_normal((experts * n, k)).astype(np.float32)).to(gpu.dev), d, block)
+    ends = None
+    if experts > 1:
+        wc, ws, ends = wc.view(experts, n, -1), ws.view(experts, n, -1), t.from_numpy(ragged(rng, rows, experts, 1 if rows > 2 else 0)).to(gpu.dev)
+    got = gpu.b.spinner_mx_linear(x, wc, ws, d, block, ends)
+    ac, as_ = gpu.b.spinner_mx_quantize(x, d, block)
+    want = gpu.b.spinner_mx_matmul(ac, as_, wc, ws, ends, x.dtype)
+    assert t.equal(got.nan_to_num(nan=12345.0), want.nan_to_num(nan=12345.0))
+    a, w = mx.values(ac.cpu().numpy(), as_.cpu().numpy()), mx.values(wc.cpu().numpy(), ws.cpu().numpy()).reshape(experts, n, k)
+    for e, (lo, hi) in enumerate(mx.bounds(None if ends is None else ends.cpu().numpy(), experts, rows)):
+        for r in range(lo, hi):
+            if r == 1:
+                assert bool(got[r].isnan().all())
+                continue
+            exact, size = t.from_numpy(w[e] @ a[r]), t.from_numpy(np.abs(w[e]) @ np.abs(a[r]))
+            check(got[r].cpu(), exact, size, (k / 64 + 64) * 2.0 ** -23, name)
+    # rows further apart, and results too
+    wide, out = t.zeros((rows, k + 5), dtype=x.dtype, device=gpu.dev), t.full((rows, n + 3), 5.0, dtype=x.dtype, device=gpu.dev)
+    wide[:, :k] = x
+    gpu.b.spinner_mx_linear(wide[:, :k], wc, ws, d, block, ends, out[:, :n])
+    assert t.equal(out[:, :n].nan_to_num(nan=12345.0), got.nan_to_num(nan=12345.0)) and bool((out[:, n:] == 5).all())
+    assert bool((gpu.b.spinner_mx_linear(x[:1].expand(rows, k), wc, ws, d, block, ends)[:1] == got[:1]).all())
