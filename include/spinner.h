@@ -464,7 +464,9 @@ int spinner_mx_matmul(const void *a_codes, const void *a_scales, long rows, int 
 /*
  * spinner_mx_quantize and spinner_mx_matmul in one call, out of the type of x:
  * a layer with 4-bit weights (quantised with the same diag and block) on plain
- * inputs.  workspace: spinner_mx_linear_workspace_bytes(rows, k) bytes.
+ * inputs.  workspace: spinner_mx_linear_workspace_bytes(rows, k) bytes; NULL will
+ * do where it is one launch: up to eight runs of 512 numbers, rows that are no
+ * multiple of 512 counted as the next one.
  */
 size_t spinner_mx_linear_workspace_bytes(long rows, int k);
 int spinner_mx_linear(const void *x, int dtype, long rows, int k, long x_stride,

@@ -995,15 +995,15 @@ int spinner_mx_linear(const void* x, int dtype, long rows, int k, long x_stride,
     if (!side(n) || !stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
     if (rows == 0) return SPINNER_OK;
     if (!w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
-    if (!workspace) return SPINNER_ERR_WORKSPACE;
     if (!aligned16(w_codes) || !aligned16(out) || !aligned16(workspace)) return SPINNER_ERR_ALIGNMENT;
     uint8_t* codes = static_cast<uint8_t*>(workspace);
-    uint8_t* scales = codes + (size_t)rows * (k / 2);
+    uint8_t* scales = codes ? codes + (size_t)rows * (k / 2) : nullptr;
     const spinner::ProductParams p = mx_params(codes, scales, rows, k, w_codes, w_scales, n, experts, ends, out, out_stride);
     if (spinner::quantises_within(p)) {
         const spinner::RawRows raw = {x, diag, x_stride, block ? 1.0f / sqrtf((float)block) : 0.0f, block ? __builtin_ctz(block) : 0};
         return launched(spinner::launch_product_raw(dtype, p, raw, static_cast<hipStream_t>(stream)));
     }
+    if (!workspace) return SPINNER_ERR_WORKSPACE;
     rc = spinner_mx_quantize(x, dtype, rows, k, x_stride, diag, block, codes, scales, stream);
     if (rc != SPINNER_OK) return rc;
     return launched(spinner::launch_product_mx4(dtype, p, static_cast<hipStream_t>(stream)));

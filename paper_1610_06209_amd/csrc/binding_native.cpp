@@ -627,9 +627,13 @@ ENTRY(mx_linear, 9)
     {
         pybind11::gil_scoped_release free;
         out = result(given, {count, n}, x->scalar_type(), *x);
-        const Tensor scratch = w.scratch(need, *x);
-        rc = spinner_mx_linear(ptr<void>(x), code, count, k, k, ptr(d), block, ptr<void>(wc), ptr<void>(ws), n, experts, ends, ptr<void>(out), n,
-                                ptr<void>(scratch), current_stream());
+        const auto call = [&](void* scratch) {
+            return spinner_mx_linear(ptr<void>(x), code, count, k, k, ptr(d), block, ptr<void>(wc), ptr<void>(ws), n, experts, ends, ptr<void>(out), n,
+                                     scratch, current_stream());
+        };
+        // a few rows need none, and making it is a tenth of such a call's time
+        rc = call(ptr<void>(w.given));
+        if (rc == SPINNER_ERR_WORKSPACE) rc = call(ptr<void>(w.scratch(need, *x)));
     }
     if (rc != SPINNER_OK) return refused(rc);
     return THPVariable_Wrap(std::move(out));

@@ -175,3 +175,17 @@ def test_layers_of_few_rows_are_quantise_then_product(gpu, name, rows, k, n, blo
     gpu.b.spinner_mx_linear(wide[:, :k], wc, ws, d, block, ends, out[:, :n])
     assert t.equal(out[:, :n].nan_to_num(nan=12345.0), got.nan_to_num(nan=12345.0)) and bool((out[:, n:] == 5).all())
     assert bool((gpu.b.spinner_mx_linear(x[:1].expand(rows, k), wc, ws, d, block, ends)[:1] == got[:1]).all())
+
+
+def test_layers_of_few_rows_need_no_workspace(gpu):
+    say("few rows, no workspace")
+    t, b = gpu.torch, gpu.b
+    d, w = t.ones(1024, device=gpu.dev), t.randn((48, 1024), device=gpu.dev)
+    wc, ws = b.spinner_mx_quantize(w, d, 1024)
+    for rows, status in ((4, b.SPINNER_OK), (5, b.SPINNER_ERR_WORKSPACE)):
+        x, out = t.randn((rows, 1024), device=gpu.dev).bfloat16(), t.full((rows, 48), 5.0, device=gpu.dev).bfloat16()
+        before = out.clone()
+        rc = b.lib.spinner_mx_linear(x.data_ptr(), 1, rows, 1024, 1024, d.data_ptr(), 1024, wc.data_ptr(), ws.data_ptr(), 48, 1, None, out.data_ptr(), 48, None,
+                                     b._stream_handle(None))
+        assert rc == status
+        assert t.equal(out, b.spinner_mx_linear(x, wc, ws, d, 1024) if rc == b.SPINNER_OK else before)
