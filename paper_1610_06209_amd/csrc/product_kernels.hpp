@@ -728,9 +728,10 @@ product_kernel(ProductParams p)
 // Up to 16 rows of a group by 16 NT columns (rows of the weights) a workgroup.  What counts is that the weights come once and at
 // the memory's rate: every wave reads its share of the depth, runs of 256 bytes of a row, straight into the registers that the
 // matrix pipe takes, one run ahead, and the four partial sums meet in LDS.
-// Measured: 24 rows over 8 experts of 8192 x 2048 in bf16 (up to 268 MB of weights) 41 us, 6.5 TB/s; 64 rows over 32 experts of 4096 x 2048 in 4 bits
-// (143 MB) 22.5 us, 6.3 TB/s; one row, 16384 x 4096 (36 MB) 8.9 us, of which the launch and the way to the first weights are half.  With runs of 64 bytes in turn
-// between the waves and scales a byte at a time: 43, 34, 11.2.
+// Measured, the same weights time after time, which the memory's cache holds / others each time: 24 rows over 8 experts of 8192 x 2048 in bf16 (268 MB) 41 /
+// 56 us, 6.5 / 4.8 TB/s; 64 rows over 32 experts of 4096 x 2048 in 4 bits (143 MB) 22.5 / 32 us, 6.3 / 4.5 TB/s; one row, 16384 x 4096 (36 MB) 8.9 us
+// of which the launch and the way to the first weights are half.  With runs of 64 bytes in turn between the waves and scales a byte at a time: 43, 34, 11.2.
+// Weights with the streaming hint, others each time: 56, 31.7; one row, 8192 x 8192 in 4 bits 11.0 for 9.8.
 constexpr int kRunSteps = 4;                              // products of a run, 64 bytes of a row each
 template <int TYPE, int NT>
 struct Run {
