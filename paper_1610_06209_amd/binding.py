@@ -217,6 +217,21 @@ def _stream_handle(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _new(shape, dtype, device, stream, scratch=False):
+    """Memory for a result, or for scratch that is let go of on return, of a call on ``stream``.
+
+    With an explicit stream it is memory of that stream: a block that the current stream has let go of may still be read or written by what
+    is queued there.  A result is then used on the current stream too.
+    """
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if not scratch:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _check_tensor(t, name, dtype):
     if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s CUDA tensor" % (name, dtype))
@@ -845,10 +860,10 @@ def _check_rows(t, name, dtype=None):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _new_or_checked(out, name, shape, dtype, like):
+def _new_or_checked(out, name, shape, dtype, like, stream):
     """A result of rows (the caller's may have rows further apart) and the distance between them."""
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=like.device)
+        out = _new(shape, dtype, like.device, stream)
     stride = _check_rows(out, name, dtype)
     if tuple(out.shape) != tuple(shape):
         raise ValueError("%s has the wrong size" % name)
@@ -886,14 +901,6 @@ def _check_rotation(diag, block, k):
     return diag.data_ptr()
 
 
-def _in_use(stream, *tensors):
-    """Tensors made here that an explicit stream works on: their memory is not given away before it has."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-
-
 def _done(rc):
     if rc != SPINNER_OK:
         raise SpinnerError(rc)
@@ -910,17 +917,15 @@ def spinner_mx_quantize(x, diag=None, block=0, codes=None, scales=None, stream=N
         return r
     stride = _check_rows(x, "x")
     rows, k = x.shape
-    given = codes is not None, scales is not None
     if codes is None:
-        codes = torch.empty((rows, k // 2), dtype=torch.uint8, device=x.device)
+        codes = _new((rows, k // 2), torch.uint8, x.device, stream)
     if scales is None:
-        scales = torch.empty((rows, k // MX4_BLOCK), dtype=torch.uint8, device=x.device)
+        scales = _new((rows, k // MX4_BLOCK), torch.uint8, x.device, stream)
     _check_bytes(codes, "codes", (rows, k // 2))
     _check_bytes(scales, "scales", (rows, k // MX4_BLOCK))
     d = _check_rotation(diag, block, k)
     _done(lib.spinner_mx_quantize(x.data_ptr(), _dtype_code(x.dtype), rows, k, stride, d, int(block), codes.data_ptr(), scales.data_ptr(),
                                    _stream_handle(stream)))
-    _in_use(stream, None if given[0] else codes, None if given[1] else scales)
     return codes, scales
 
 
@@ -934,10 +939,8 @@ def spinner_mx_dequantize(codes, scales, dtype=torch.float32, out=None, stream=N
     _check_bytes(codes, "codes", (rows, k // 2))
     _check_bytes(scales, "scales", (rows, k // MX4_BLOCK))
     code = _dtype_code(dtype)
-    made = out is None
-    out, stride = _new_or_checked(out, "out", (rows, k), dtype, codes)
+    out, stride = _new_or_checked(out, "out", (rows, k), dtype, codes, stream)
     _done(lib.spinner_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, out.data_ptr(), code, stride, _stream_handle(stream)))
-    _in_use(stream, out if made else None)
     return out
 
 
@@ -959,11 +962,9 @@ def spinner_mx_matmul(a_codes, a_scales, w_codes, w_scales, ends=None, dtype=tor
     _check_bytes(w_scales, "w_scales", (*w_codes.shape[:-1], k // MX4_BLOCK))
     e = _check_ends(ends, experts, "w_codes")
     code = _dtype_code(dtype)
-    made = out is None
-    out, stride = _new_or_checked(out, "out", (rows, n), dtype, a_codes)
+    out, stride = _new_or_checked(out, "out", (rows, n), dtype, a_codes, stream)
     _done(lib.spinner_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), rows, k, w_codes.data_ptr(), w_scales.data_ptr(), n, experts, e,
                                  out.data_ptr(), code, stride, _stream_handle(stream)))
-    _in_use(stream, out if made else None)
     return out
 
 
@@ -987,15 +988,13 @@ def spinner_mx_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, out=N
     _check_bytes(w_scales, "w_scales", (*w_codes.shape[:-1], k // MX4_BLOCK))
     d = _check_rotation(diag, block, k)
     e = _check_ends(ends, experts, "w_codes")
-    made = out is None, workspace is None
-    out, stride = _new_or_checked(out, "out", (rows, n), x.dtype, x)
+    out, stride = _new_or_checked(out, "out", (rows, n), x.dtype, x, stream)
     need = spinner_mx_linear_workspace_bytes(rows, k)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     _done(lib.spinner_mx_linear(x.data_ptr(), code, rows, k, x_stride, d, int(block), w_codes.data_ptr(), w_scales.data_ptr(), n, experts, e,
                                  out.data_ptr(), stride, workspace.data_ptr(), _stream_handle(stream)))
-    _in_use(stream, out if made[0] else None, workspace if made[1] else None)
     return out
 
 
@@ -1006,11 +1005,9 @@ def _grouped(call, a, w, ends, out, stream, across):
     if w.dtype != a.dtype or a.shape[1] != (k if across else n):
         raise ValueError("w must be of the type and width of the rows")
     e = _check_ends(ends, experts, "w")
-    made = out is None
-    out, stride = _new_or_checked(out, "out" if across else "dx", (a.shape[0], n if across else k), a.dtype, a)
+    out, stride = _new_or_checked(out, "out" if across else "dx", (a.shape[0], n if across else k), a.dtype, a, stream)
     depth, width = (k, n) if across else (n, k)
     _done(call(a.data_ptr(), code, a.shape[0], depth, a_stride, w.data_ptr(), width, experts, e, out.data_ptr(), stride, _stream_handle(stream)))
-    _in_use(stream, out if made else None)
     return out
 
 
@@ -1049,17 +1046,15 @@ def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, wo
     experts = 1 if ends is None else ends.numel()
     e = _check_ends(ends, experts, "dw")
     shape = (n, k) if ends is None else (experts, n, k)
-    made = dw is None, workspace is None
     if dw is None:
-        dw = torch.empty(shape, dtype=dtype, device=dy.device)
+        dw = _new(shape, dtype, dy.device, stream)
     _check_here(dw, "dw", dtype)
     if tuple(dw.shape) != shape or not dw.is_contiguous():
         raise ValueError("dw must be contiguous, of shape %s" % (shape,))
     need = spinner_grouped_matmul_dw_workspace_bytes(rows, n, k, experts)
     if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        workspace = _new(need, torch.uint8, dy.device, stream, scratch=True)
     _check_workspace(workspace, need)
     _done(lib.spinner_grouped_matmul_dw(dy.data_ptr(), x.data_ptr(), code, rows, n, k, dy_stride, x_stride, experts, e, dw.data_ptr(), dw_code,
                                         workspace.data_ptr() if workspace is not None else None, _stream_handle(stream)))
-    _in_use(stream, dw if made[0] else None, workspace if made[1] else None)
     return dw

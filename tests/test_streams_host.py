@@ -1,0 +1,88 @@
+"""Where the memory comes from that a call makes for itself when it is given a stream: from that stream, whatever the current one has queued
+on blocks that it let go of.  On the host, with tensors that are only described and a library that launches nothing."""
+import contextlib
+
+import pytest
+
+from test_abi_host import _NoLaunch, _Tensor
+
+MINE = type("Stream", (), {"cuda_stream": 4096})()
+CURRENT = type("Stream", (), {"cuda_stream": 0})()
+
+
+class _OnGpu(_Tensor):
+    def __init__(self, *shape, dtype="float32", made_on=None):
+        import torch
+
+        super().__init__(*shape, dtype=dtype)
+        self.device, self.made_on, self.used_on = torch.device("cuda:0"), made_on, []
+
+    def stride(self, i):
+        return 1 if i else self.shape[1]
+
+    def untyped_storage(self):
+        return type("Storage", (), {"nbytes": lambda _, n=self.numel() * self.element_size(): n})()
+
+    def record_stream(self, stream):
+        self.used_on.append(stream)
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """Every tensor that is made, with the stream that was current then; the binding without launches."""
+    import torch
+
+    from paper_1610_06209_amd import binding as b
+
+    tensors, streams = [], [CURRENT]
+
+    def empty(*shape, dtype=torch.float32, device=None):
+        shape = shape[0] if len(shape) == 1 and not isinstance(shape[0], int) else shape
+        tensors.append(_OnGpu(*shape, dtype=str(dtype)[6:], made_on=streams[-1]))
+        return tensors[-1]
+
+    @contextlib.contextmanager
+    def on(stream):
+        streams.append(stream)
+        yield
+        streams.pop()
+
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch, "empty_like", lambda t: empty(*t.shape, dtype=t.dtype))
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: streams[-1])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(b, "lib", _NoLaunch(b.lib))
+    monkeypatch.setattr(b, "_stream_handle", lambda stream: (stream or streams[-1]).cuda_stream)
+    return b, tensors
+
+
+T, u8, h = _OnGpu, dict(dtype="uint8"), dict(dtype="bfloat16")
+CALLS = {
+    "spinner_mx_quantize": dict(x=T(5, 128)),
+    "spinner_mx_dequantize": dict(codes=T(5, 64, **u8), scales=T(5, 4, **u8)),
+    "spinner_mx_matmul": dict(a_codes=T(5, 64, **u8), a_scales=T(5, 4, **u8), w_codes=T(7, 64, **u8), w_scales=T(7, 4, **u8)),
+    "spinner_mx_linear": dict(x=T(5, 128, **h), w_codes=T(7, 64, **u8), w_scales=T(7, 4, **u8)),
+    "spinner_grouped_matmul": dict(x=T(5, 128, **h), w=T(7, 128, **h)),
+    "spinner_grouped_matmul_dx": dict(dy=T(5, 7, **h), w=T(7, 128, **h)),
+    "spinner_grouped_matmul_dw": dict(dy=T(4100, 40, **h), x=T(4100, 264, **h)),           # (sums in shares: with a workspace)
+}
+SCRATCH = {"spinner_mx_linear": 1, "spinner_grouped_matmul_dw": 1}                        # tensors made and not returned
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_memory_comes_from_the_stream_of_the_call(made, name):
+    b, tensors = made
+    r = getattr(b, name)(stream=MINE, **CALLS[name])
+    results = r if isinstance(r, tuple) else (r,)
+    assert tensors and all(t.made_on is MINE for t in tensors)
+    assert len(tensors) == len(results) + SCRATCH.get(name, 0)
+    # results are used by the caller afterwards, on the stream that is current there
+    assert all(t.used_on == ([CURRENT] if any(t is q for q in results) else []) for t in tensors)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_memory_of_other_calls_comes_from_the_current_stream(made, name):
+    b, tensors = made
+    getattr(b, name)(**CALLS[name])
+    assert tensors and all(t.made_on is CURRENT and not t.used_on for t in tensors)
