@@ -228,7 +228,7 @@ def _new(shape, dtype, device, stream, scratch=False):
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     if not scratch:
-        t.record_stream(torch.cuda.current_stream())
+        t.record_stream(torch.cuda.current_stream(device))
     return t
 
 
@@ -292,14 +292,14 @@ def spinner_apply(x, d1, d2, d3, m=None, epilogue="none", scale=1.0, out=None, w
     epi = _epi(epilogue)
     width = 2 * m if epi == SPINNER_EPI_COSSIN else m
     if out is None:
-        out = torch.empty((batch, width), dtype=torch.float32, device=x.device)
+        out = _new((batch, width), torch.float32, x.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != batch * width:
             raise ValueError("out has the wrong size")
     need = spinner_workspace_bytes(n, batch, m, epi)
     if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_apply(x.data_ptr(), n, batch, d1.data_ptr(), d2.data_ptr(), d3.data_ptr(), m, epi,
                            ctypes.c_float(scale), out.data_ptr(),
@@ -321,7 +321,7 @@ def spinner_hash(x, diag_sets, out_idx=None, stream=None):
         raise ValueError("diag_sets must be [L][3][n]")
     L = diag_sets.shape[0]
     if out_idx is None:
-        out_idx = torch.empty((batch, L), dtype=torch.int32, device=x.device)
+        out_idx = _new((batch, L), torch.int32, x.device, stream)
     else:
         _check_tensor(out_idx, "out_idx", torch.int32)
         if out_idx.numel() != batch * L:
@@ -336,10 +336,10 @@ def spinner_hash_workspace_bytes(n: int, batch: int) -> int:
     return int(lib.spinner_hash_workspace_bytes(int(n), int(batch)))
 
 
-def _hash_workspace(x, n, batch, workspace):
+def _hash_workspace(x, n, batch, workspace, stream):
     need = spinner_hash_workspace_bytes(n, batch)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     return workspace
 
@@ -353,12 +353,12 @@ def spinner_hash_ws(x, diag_sets, out_idx=None, workspace=None, stream=None):
         raise ValueError("diag_sets must be [L][3][n]")
     L = diag_sets.shape[0]
     if out_idx is None:
-        out_idx = torch.empty((batch, L), dtype=torch.int32, device=x.device)
+        out_idx = _new((batch, L), torch.int32, x.device, stream)
     else:
         _check_tensor(out_idx, "out_idx", torch.int32)
         if out_idx.numel() != batch * L:
             raise ValueError("out_idx has the wrong size")
-    workspace = _hash_workspace(x, n, batch, workspace)
+    workspace = _hash_workspace(x, n, batch, workspace, stream)
     rc = lib.spinner_hash_ws(x.data_ptr(), n, batch, L, diag_sets.data_ptr(), out_idx.data_ptr(),
                              workspace.data_ptr() if workspace is not None else None, _stream_handle(stream))
     if rc != SPINNER_OK:
@@ -372,12 +372,12 @@ def spinner_hash_signs_ws(x, signs, L, out_idx=None, workspace=None, stream=None
     batch, n = x.shape
     _check_signs(signs, n, L)
     if out_idx is None:
-        out_idx = torch.empty((batch, L), dtype=torch.int32, device=x.device)
+        out_idx = _new((batch, L), torch.int32, x.device, stream)
     else:
         _check_tensor(out_idx, "out_idx", torch.int32)
         if out_idx.numel() != batch * L:
             raise ValueError("out_idx has the wrong size")
-    workspace = _hash_workspace(x, n, batch, workspace)
+    workspace = _hash_workspace(x, n, batch, workspace, stream)
     rc = lib.spinner_hash_signs_ws(x.data_ptr(), n, batch, L, signs.data_ptr(), out_idx.data_ptr(),
                                    workspace.data_ptr() if workspace is not None else None, _stream_handle(stream))
     if rc != SPINNER_OK:
@@ -398,7 +398,7 @@ def spinner_pack_signs(diag_sets, stream=None):
     nbytes = spinner_signs_bytes(n, L)
     if nbytes == 0:
         raise SpinnerError(SPINNER_ERR_BAD_N)
-    signs = torch.empty(nbytes, dtype=torch.uint8, device=diag_sets.device)
+    signs = _new(nbytes, torch.uint8, diag_sets.device, stream)
     rc = lib.spinner_pack_signs(diag_sets.data_ptr(), n, L, signs.data_ptr(), _stream_handle(stream))
     if rc != SPINNER_OK:
         raise SpinnerError(rc)
@@ -417,7 +417,7 @@ def spinner_apply_signs(x, signs, m=None, epilogue="none", scale=1.0, out=None, 
     epi = _epi(epilogue)
     width = 2 * m if epi == SPINNER_EPI_COSSIN else m
     if out is None:
-        out = torch.empty((batch, width), dtype=torch.float32, device=x.device)
+        out = _new((batch, width), torch.float32, x.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != batch * width:
@@ -426,7 +426,7 @@ def spinner_apply_signs(x, signs, m=None, epilogue="none", scale=1.0, out=None, 
     _check_signs(signs, n, 1, triple)
     need = spinner_workspace_bytes(n, batch, m, epi)
     if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_apply_signs(x.data_ptr(), n, batch, signs.data_ptr() + triple * one, m, epi,
                                  ctypes.c_float(scale), out.data_ptr(),
@@ -445,7 +445,7 @@ def spinner_hash_signs(x, signs, L, out_idx=None, stream=None):
     batch, n = x.shape
     _check_signs(signs, n, L)
     if out_idx is None:
-        out_idx = torch.empty((batch, L), dtype=torch.int32, device=x.device)
+        out_idx = _new((batch, L), torch.int32, x.device, stream)
     else:
         _check_tensor(out_idx, "out_idx", torch.int32)
         if out_idx.numel() != batch * L:
@@ -485,13 +485,13 @@ def spinner_code_position(coordinate: int):
     return w.value, b.value
 
 
-def _codes_out(x, m, codes):
+def _codes_out(x, m, codes, stream):
     batch = x.shape[0]
     nbytes = spinner_code_bytes(m)
     if nbytes == 0:
         raise SpinnerError(SPINNER_ERR_BAD_M)
     if codes is None:
-        codes = torch.empty((batch, nbytes // 8), dtype=torch.int64, device=x.device)
+        codes = _new((batch, nbytes // 8), torch.int64, x.device, stream)
     else:
         _check_tensor(codes, "codes", torch.int64)
         if codes.numel() != batch * (nbytes // 8):
@@ -499,11 +499,11 @@ def _codes_out(x, m, codes):
     return codes
 
 
-def _codes_workspace(x, workspace):
+def _codes_workspace(x, workspace, stream):
     batch, n = x.shape
     need = spinner_codes_workspace_bytes(n, batch)
     if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     return workspace
 
@@ -517,8 +517,8 @@ def spinner_sign_codes(x, d1, d2, d3, m=None, codes=None, workspace=None, stream
     batch, n = x.shape
     _check_diagonals(n, d1=d1, d2=d2, d3=d3)
     m = n if m is None else int(m)
-    codes = _codes_out(x, m, codes)
-    workspace = _codes_workspace(x, workspace)
+    codes = _codes_out(x, m, codes, stream)
+    workspace = _codes_workspace(x, workspace, stream)
     rc = lib.spinner_sign_codes(x.data_ptr(), n, batch, d1.data_ptr(), d2.data_ptr(), d3.data_ptr(), m, codes.data_ptr(),
                                 workspace.data_ptr() if workspace is not None else None, _stream_handle(stream))
     if rc != SPINNER_OK:
@@ -534,8 +534,8 @@ def spinner_sign_codes_signs(x, signs, m=None, codes=None, workspace=None, strea
     _check_tensor(x, "x", torch.float32)
     batch, n = x.shape
     m = n if m is None else int(m)
-    codes = _codes_out(x, m, codes)
-    workspace = _codes_workspace(x, workspace)
+    codes = _codes_out(x, m, codes, stream)
+    workspace = _codes_workspace(x, workspace, stream)
     one = spinner_signs_bytes(n, 1)
     _check_signs(signs, n, 1, triple)
     rc = lib.spinner_sign_codes_signs(x.data_ptr(), n, batch, signs.data_ptr() + triple * one, m, codes.data_ptr(),
@@ -561,7 +561,7 @@ def spinner_angular_gram(codes_a, codes_b, m, out=None, stream=None):
     if codes_a.numel() < na * words or codes_b.numel() < nb * words:
         raise ValueError("codes do not have m / 64 words per row")
     if out is None:
-        out = torch.empty((na, nb), dtype=torch.float32, device=codes_a.device)
+        out = _new((na, nb), torch.float32, codes_a.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != na * nb:
@@ -590,12 +590,12 @@ def spinner_layer_forward(x, d1, d2, d3, scale=1.0, y=None, saved=None, stream=N
     batch, n = x.shape
     _check_diagonals(n, d1=d1, d2=d2, d3=d3)
     if y is None:
-        y = torch.empty_like(x)
+        y = _new(x.shape, torch.float32, x.device, stream)
     else:
         _check_tensor(y, "y", torch.float32)
         _check_result(y, "y", batch * n)
     if saved is None:
-        saved = torch.empty((2, batch, n), dtype=torch.float32, device=x.device)
+        saved = _new((2, batch, n), torch.float32, x.device, stream)
     else:
         _check_tensor(saved, "saved", torch.float32)
         if saved.numel() != 2 * batch * n:
@@ -619,16 +619,16 @@ def spinner_layer_backward(dy, x, saved, d1, d2, d3, scale=1.0, dx=None, dd=None
     if dy.shape != x.shape or saved.numel() != 2 * batch * n:
         raise ValueError("dy / saved do not match x")
     if dx is None:
-        dx = torch.empty_like(x)
+        dx = _new(x.shape, torch.float32, x.device, stream)
     else:
         _check_result(dx, "dx", batch * n)
     if dd is None:
-        dd = torch.empty((3, n), dtype=torch.float32, device=x.device)
+        dd = _new((3, n), torch.float32, x.device, stream)
     else:
         _check_result(dd, "dd", 3 * n)
     need = spinner_layer_workspace_bytes(n, batch)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+        workspace = _new(max(need, 16), torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_layer_backward(dy.data_ptr(), x.data_ptr(), saved.data_ptr(), n, batch, d1.data_ptr(), d2.data_ptr(),
                                     d3.data_ptr(), ctypes.c_float(scale), dx.data_ptr(), dd.data_ptr(), workspace.data_ptr(),
@@ -653,14 +653,14 @@ def spinner_sketch(A, w, d1, d2, d3, m, scale=1.0, out=None, workspace=None, str
     if w is not None:
         _check_diagonals(n, w=w)
     if out is None:
-        out = torch.empty((int(m), d), dtype=torch.float32, device=A.device)
+        out = _new((int(m), d), torch.float32, A.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != int(m) * d:
             raise ValueError("out has the wrong size")
     need = spinner_sketch_workspace_bytes(n, d, m)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=A.device)
+        workspace = _new(max(need, 16), torch.uint8, A.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_sketch(A.data_ptr(), n, d, w.data_ptr() if w is not None else None, d1.data_ptr(), d2.data_ptr(),
                             d3.data_ptr(), int(m), ctypes.c_float(scale), out.data_ptr(), workspace.data_ptr(),
@@ -699,14 +699,14 @@ def spinner_sketch_gram(B, out=None, workspace=None, stream=None):
     _check_tensor(B, "B", torch.float32)
     m, d = B.shape
     if out is None:
-        out = torch.empty((d, d), dtype=torch.float32, device=B.device)
+        out = _new((d, d), torch.float32, B.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != d * d:
             raise ValueError("out has the wrong size")
     need = spinner_sketch_gram_workspace_bytes(m, d)
     if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=B.device)
+        workspace = _new(need, torch.uint8, B.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_sketch_gram(B.data_ptr(), m, d, out.data_ptr(), workspace.data_ptr() if workspace is not None else None,
                                  _stream_handle(stream))
@@ -731,14 +731,14 @@ def spinner_apply_blocks(x, diag_sets, m=None, epilogue="none", scale=1.0, out=N
     epi = _epi(epilogue)
     width = (2 * m if epi == SPINNER_EPI_COSSIN else m) * L
     if out is None:
-        out = torch.empty((batch, width), dtype=torch.float32, device=x.device)
+        out = _new((batch, width), torch.float32, x.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != batch * width:
             raise ValueError("out has the wrong size")
     need = int(lib.spinner_blocks_workspace_bytes(n, batch, m, epi))
     if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_apply_blocks(x.data_ptr(), n, batch, L, diag_sets.data_ptr(), m, epi, ctypes.c_float(scale),
                                   out.data_ptr(), workspace.data_ptr() if workspace is not None else None,
@@ -757,7 +757,7 @@ def spinner_struct_prepare(kind, params, n, stream=None):
         raise SpinnerError(SPINNER_ERR_UNSUPPORTED)
     if params.numel() != int(lib.spinner_struct_params(k, int(n))):
         raise ValueError("generating vector has the wrong length")
-    spec = torch.empty(nbytes, dtype=torch.uint8, device=params.device)
+    spec = _new(nbytes, torch.uint8, params.device, stream)
     rc = lib.spinner_struct_prepare(k, params.data_ptr(), int(n), spec.data_ptr(), _stream_handle(stream))
     if rc != SPINNER_OK:
         raise SpinnerError(rc)
@@ -779,7 +779,7 @@ def spinner_struct_apply(x, kind, spectrum, d1, d2, m=None, scale=1.0, out=None,
     _check_spectrum(spectrum, k, n)
     m = n if m is None else int(m)
     if out is None:
-        out = torch.empty((batch, m), dtype=torch.float32, device=x.device)
+        out = _new((batch, m), torch.float32, x.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != batch * m:
@@ -808,14 +808,14 @@ def spinner_struct_apply_ws(x, kind, spectrum, d1, d2, m=None, scale=1.0, out=No
     _check_spectrum(spectrum, k, n)
     m = n if m is None else int(m)
     if out is None:
-        out = torch.empty((batch, m), dtype=torch.float32, device=x.device)
+        out = _new((batch, m), torch.float32, x.device, stream)
     else:
         _check_tensor(out, "out", torch.float32)
         if out.numel() != batch * m:
             raise ValueError("out has the wrong size")
     need = spinner_struct_workspace_bytes(k, n, batch)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
     _check_workspace(workspace, need)
     rc = lib.spinner_struct_apply_ws(x.data_ptr(), n, batch, k, spectrum.data_ptr(), d1.data_ptr(), d2.data_ptr(), m,
                                      ctypes.c_float(scale), out.data_ptr(),

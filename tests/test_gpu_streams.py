@@ -117,3 +117,49 @@ def test_results_of_a_stream_outlive_what_the_current_one_reads_of_them(gpu):
     t.cuda.synchronize()
     assert all(t.equal(p, q) for p, q in zip(reads, wants))
     assert np.isfinite(reads[0].cpu().numpy()).all()
+
+
+def transform_calls(g):
+    t, b = g.torch, g.b
+    gen = t.Generator(device=g.dev)
+    gen.manual_seed(4)
+    n, wide = 1 << 12, 1 << 17
+    x, xw = t.randn((300, n), generator=gen, device=g.dev), t.randn((9, wide), generator=gen, device=g.dev)
+    d, dw = (t.randint(0, 2, (2, 3, s), generator=gen, device=g.dev).float() * 2 - 1 for s in (n, wide))
+    signs, signs_w = b.spinner_pack_signs(d), b.spinner_pack_signs(dw)
+    codes = b.spinner_sign_codes(x, *d[0])
+    y, saved = b.spinner_layer_forward(x, *d[0], 0.5)
+    gp = t.randn(n, generator=gen, device=g.dev)
+    spectrum = b.spinner_struct_prepare("circulant", gp, n)
+    A = t.randn((n, 60), generator=gen, device=g.dev)
+    t.cuda.synchronize()
+    return {
+        "apply": lambda **k: b.spinner_apply(xw, *dw[0], 100, **k),
+        "apply_signs": lambda **k: b.spinner_apply_signs(xw, signs_w, 100, **k),
+        "apply_blocks": lambda **k: b.spinner_apply_blocks(x, d, 512, "cossin", 3.0, **k),
+        "pack_signs": lambda **k: b.spinner_pack_signs(d, **k),
+        "hash": lambda **k: b.spinner_hash(x, d, **k),
+        "hash_signs": lambda **k: b.spinner_hash_signs(x, signs, 2, **k),
+        "hash_ws": lambda **k: b.spinner_hash_ws(xw, dw, **k),
+        "hash_signs_ws": lambda **k: b.spinner_hash_signs_ws(xw, signs_w, 2, **k),
+        "sign_codes": lambda **k: b.spinner_sign_codes(xw, *dw[0], **k),
+        "sign_codes_signs": lambda **k: b.spinner_sign_codes_signs(x, signs, **k),
+        "angular_gram": lambda **k: b.spinner_angular_gram(codes, codes[:50], n, **k),
+        "layer_forward": lambda **k: b.spinner_layer_forward(x, *d[0], 0.5, **k),
+        "layer_backward": lambda **k: b.spinner_layer_backward(y, x, saved, *d[0], 0.5, **k),
+        "sketch": lambda **k: b.spinner_sketch(A, None, *d[0], 128, **k),
+        "sketch_gram": lambda **k: b.spinner_sketch_gram(A, **k),
+        "struct_prepare": lambda **k: b.spinner_struct_prepare("circulant", gp, n, **k),
+        "struct_apply": lambda **k: b.spinner_struct_apply(x, "circulant", spectrum, *d[0, :2], **k),
+        "struct_apply_ws": lambda **k: b.spinner_struct_apply_ws(x, "circulant", spectrum, *d[0, :2], **k),
+    }
+
+
+TRANSFORMS = ["apply", "apply_signs", "apply_blocks", "pack_signs", "hash", "hash_signs", "hash_ws", "hash_signs_ws", "sign_codes", "sign_codes_signs", "angular_gram",
+              "layer_forward", "layer_backward", "sketch", "sketch_gram", "struct_prepare", "struct_apply", "struct_apply_ws"]
+
+
+@pytest.mark.parametrize("name", TRANSFORMS)
+def test_transforms_on_a_stream_of_their_own(gpu, name, monkeypatch):
+    say("stream of its own", name)
+    check_call(gpu, transform_calls(gpu)[name], monkeypatch)

@@ -50,7 +50,7 @@ def made(monkeypatch):
     monkeypatch.setattr(torch, "empty", empty)
     monkeypatch.setattr(torch, "empty_like", lambda t: empty(*t.shape, dtype=t.dtype))
     monkeypatch.setattr(torch.cuda, "stream", on)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda: streams[-1])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *device: streams[-1])
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(b, "lib", _NoLaunch(b.lib))
     monkeypatch.setattr(b, "_stream_handle", lambda stream: (stream or streams[-1]).cuda_stream)
@@ -67,7 +67,33 @@ CALLS = {
     "spinner_grouped_matmul_dx": dict(dy=T(5, 7, **h), w=T(7, 128, **h)),
     "spinner_grouped_matmul_dw": dict(dy=T(4100, 40, **h), x=T(4100, 264, **h)),           # (sums in shares: with a workspace)
 }
-SCRATCH = {"spinner_mx_linear": 1, "spinner_grouped_matmul_dw": 1}                        # tensors made and not returned
+# the other entry points, at sizes where they make scratch memory if they ever do
+_n, _wide, _d3 = 1 << 15, 1 << 17, lambda n: dict(d1=T(n), d2=T(n), d3=T(n))              # noqa: E731
+_signs = lambda n, L: T(1 << 20, **u8)                                                    # noqa: E731
+CALLS.update({
+    "spinner_apply": dict(x=T(3, _wide), m=100, **_d3(_wide)),
+    "spinner_apply_signs": dict(x=T(3, _wide), signs=_signs(_wide, 1), m=100),
+    "spinner_apply_blocks": dict(x=T(3, _wide), diag_sets=T(2, 3, _wide), m=100),
+    "spinner_pack_signs": dict(diag_sets=T(2, 3, _n)),
+    "spinner_hash": dict(x=T(3, _n), diag_sets=T(2, 3, _n)),
+    "spinner_hash_signs": dict(x=T(3, _n), signs=_signs(_n, 2), L=2),
+    "spinner_hash_ws": dict(x=T(3, _wide), diag_sets=T(2, 3, _wide)),
+    "spinner_hash_signs_ws": dict(x=T(3, _wide), signs=_signs(_wide, 2), L=2),
+    "spinner_sign_codes": dict(x=T(3, _wide), **_d3(_wide)),
+    "spinner_sign_codes_signs": dict(x=T(3, _wide), signs=_signs(_wide, 1)),
+    "spinner_angular_gram": dict(codes_a=T(5, 4, dtype="int64"), codes_b=T(3, 4, dtype="int64"), m=256),
+    "spinner_layer_forward": dict(x=T(3, _n), **_d3(_n)),
+    "spinner_layer_backward": dict(dy=T(3, _n), x=T(3, _n), saved=T(2, 3, _n), **_d3(_n)),
+    "spinner_sketch": dict(A=T(_n, 20), w=None, m=64, **_d3(_n)),
+    "spinner_sketch_gram": dict(B=T(4096, 200)),
+    "spinner_struct_prepare": dict(kind="circulant", params=T(_n), n=_n),
+    "spinner_struct_apply": dict(x=T(3, 1 << 12), kind="circulant", spectrum=_signs(0, 0), d1=T(1 << 12), d2=T(1 << 12)),
+    "spinner_struct_apply_ws": dict(x=T(3, _n), kind="circulant", spectrum=_signs(0, 0), d1=T(_n), d2=T(_n)),
+})
+# tensors made and not returned
+SCRATCH = {name: 1 for name in ("spinner_mx_linear", "spinner_grouped_matmul_dw", "spinner_apply", "spinner_apply_signs", "spinner_apply_blocks", "spinner_hash_ws",
+                                "spinner_hash_signs_ws", "spinner_sign_codes", "spinner_sign_codes_signs", "spinner_layer_backward", "spinner_sketch", "spinner_sketch_gram",
+                                "spinner_struct_apply_ws")}
 
 
 @pytest.mark.parametrize("name", list(CALLS))
