@@ -837,6 +837,16 @@ def _dtype_code(dtype):
     return DTYPES[dtype]
 
 
+def _fits(*numbers):
+    """Whether numbers are as many as the C ABI's int holds; ctypes would cut them off."""
+    return all(-1 << 31 <= v < 1 << 31 for v in numbers)
+
+
+def _check_sizes(*numbers):
+    if not _fits(*numbers):
+        raise SpinnerError(SPINNER_ERR_BAD_SHAPE)
+
+
 def _check_here(t, name, dtype=None, dim=None):
     """A tensor of the expected type and number of dimensions on the GPU that the call runs on."""
     if not t.is_cuda or (dtype is not None and t.dtype != dtype) or (dim is not None and t.dim() != dim):
@@ -917,6 +927,7 @@ def spinner_mx_quantize(x, diag=None, block=0, codes=None, scales=None, stream=N
         return r
     stride = _check_rows(x, "x")
     rows, k = x.shape
+    _check_sizes(k, int(block))
     if codes is None:
         codes = _new((rows, k // 2), torch.uint8, x.device, stream)
     if scales is None:
@@ -936,6 +947,7 @@ def spinner_mx_dequantize(codes, scales, dtype=torch.float32, out=None, stream=N
         return r
     _check_here(codes, "codes", torch.uint8, 2)
     rows, k = codes.shape[0], 2 * codes.shape[1]
+    _check_sizes(k)
     _check_bytes(codes, "codes", (rows, k // 2))
     _check_bytes(scales, "scales", (rows, k // MX4_BLOCK))
     code = _dtype_code(dtype)
@@ -958,6 +970,7 @@ def spinner_mx_matmul(a_codes, a_scales, w_codes, w_scales, ends=None, dtype=tor
     _check_bytes(a_codes, "a_codes", (rows, k // 2))
     _check_bytes(a_scales, "a_scales", (rows, k // MX4_BLOCK))
     experts, n, _ = _check_weights(w_codes, "w_codes")
+    _check_sizes(k, n, experts)
     _check_bytes(w_codes, "w_codes", (*w_codes.shape[:-1], k // 2))
     _check_bytes(w_scales, "w_scales", (*w_codes.shape[:-1], k // MX4_BLOCK))
     e = _check_ends(ends, experts, "w_codes")
@@ -969,7 +982,7 @@ def spinner_mx_matmul(a_codes, a_scales, w_codes, w_scales, ends=None, dtype=tor
 
 
 def spinner_mx_linear_workspace_bytes(rows: int, k: int) -> int:
-    return int(lib.spinner_mx_linear_workspace_bytes(int(rows), int(k)))
+    return int(lib.spinner_mx_linear_workspace_bytes(int(rows), int(k))) if _fits(int(k)) else 0
 
 
 def spinner_mx_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, out=None, workspace=None, stream=None):
@@ -984,6 +997,7 @@ def spinner_mx_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, out=N
     code = _dtype_code(x.dtype)
     rows, k = x.shape
     experts, n, _ = _check_weights(w_codes, "w_codes")
+    _check_sizes(k, n, experts, int(block))
     _check_bytes(w_codes, "w_codes", (*w_codes.shape[:-1], k // 2))
     _check_bytes(w_scales, "w_scales", (*w_codes.shape[:-1], k // MX4_BLOCK))
     d = _check_rotation(diag, block, k)
@@ -1002,6 +1016,7 @@ def _grouped(call, a, w, ends, out, stream, across):
     a_stride = _check_rows(a, "x" if across else "dy")
     code = _dtype_code(a.dtype)
     experts, n, k = _check_weights(w, "w")
+    _check_sizes(experts, n, k)
     if w.dtype != a.dtype or a.shape[1] != (k if across else n):
         raise ValueError("w must be of the type and width of the rows")
     e = _check_ends(ends, experts, "w")
@@ -1027,7 +1042,7 @@ def spinner_grouped_matmul_dx(dy, w, ends=None, dx=None, stream=None):
 
 
 def spinner_grouped_matmul_dw_workspace_bytes(rows: int, n: int, k: int, experts: int) -> int:
-    return int(lib.spinner_grouped_matmul_dw_workspace_bytes(int(rows), int(n), int(k), int(experts)))
+    return int(lib.spinner_grouped_matmul_dw_workspace_bytes(int(rows), int(n), int(k), int(experts))) if _fits(int(n), int(k), int(experts)) else 0
 
 
 def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, workspace=None, stream=None):
@@ -1044,6 +1059,7 @@ def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, wo
     if x.shape[0] != rows:
         raise ValueError("dy and x must have as many rows")
     experts = 1 if ends is None else ends.numel()
+    _check_sizes(n, k, experts)
     e = _check_ends(ends, experts, "dw")
     shape = (n, k) if ends is None else (experts, n, k)
     if dw is None:
