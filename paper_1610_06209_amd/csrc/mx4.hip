@@ -58,11 +58,11 @@ __global__ void __launch_bounds__(LOG > 9 ? 64 * waves_of_run(LOG) : 256) mx4_qu
 
 // Codes back to numbers, 16 bytes of them a thread (STRIDED: rows of `out` that do not follow one another).  bf16 16384 x 16384 128 us, 5.3 TB/s.
 template <typename T, bool STRIDED>
-__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long pieces,
+__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long first, long long pieces,
                                                              int row_pieces, T* __restrict__ out, long long out_stride)
 {
     constexpr int M = 16 / sizeof(T);
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long i = first + (long long)blockIdx.x * 256 + threadIdx.x;
     if (i >= pieces) return;
     const unsigned code = M == 8 ? reinterpret_cast<const unsigned*>(codes)[i] : reinterpret_cast<const unsigned short*>(codes)[i];
     const int byte = scales[i / (32 / M)];
@@ -121,11 +121,16 @@ hipError_t dequantize(const uint8_t* codes, const uint8_t* scales, int rows, int
 {
     constexpr int numbers = 16 / sizeof(T);
     const long long pieces = (long long)rows * (k / numbers);
-    const long long blocks = (pieces + 255) / 256;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const auto kernel = out_stride == k || rows == 1 ? mx4_dequantize_kernel<T, false> : mx4_dequantize_kernel<T, true>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, pieces, k / numbers, static_cast<T*>(out), out_stride);
-    return hipGetLastError();
+    // in grids of fewer than 2^32 threads
+    constexpr long long most = 1LL << 31;
+    for (long long first = 0; first < pieces; first += most) {
+        const long long threads = pieces - first < most ? pieces - first : most;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, codes, scales, first, pieces, k / numbers, static_cast<T*>(out), out_stride);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

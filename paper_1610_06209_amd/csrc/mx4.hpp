@@ -41,6 +41,7 @@ struct ProductParams {
     long long b_group;                    // kForward, kDx: bytes from one expert's weights to the next
     long long out_stride;                 // elements from one row of the result to the next
     int rows, experts;
+    unsigned first_block;                 // (kernels) workgroup 0 of this grid in the order of all
     int height;                           // kDw: rows of one expert's result
     int width;                            // columns of the result
     int depth;                            // kForward, kDx: numbers in a sum

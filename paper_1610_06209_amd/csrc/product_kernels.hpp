@@ -393,7 +393,7 @@ product_kernel(ProductParams p)
     if constexpr (DIRECTION == kDw) {
         // an equal share of every expert's tiles to each XCD: the depth of an expert's sums is the number of its rows
         const unsigned per_expert = columns * ((unsigned)(p.height + BM - 1) / BM), share = (per_expert + 7) / 8;
-        const unsigned k = blockIdx.x >> 3, expert = k / share, tile = (blockIdx.x & 7) * share + k % share;
+        const unsigned block = p.first_block + blockIdx.x, k = block >> 3, expert = k / share, tile = (block & 7) * share + k % share;
         if (tile >= per_expert) return;
         int lo = 0, hi = p.rows;
         if (p.ends) {
@@ -418,7 +418,7 @@ product_kernel(ProductParams p)
     } else {
         RowTiles<BM> tiles(p);
         unsigned tile;
-        if (!xcd_run(blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
+        if (!xcd_run(p.first_block + blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
         // bands of four row tiles, column by column
         const unsigned band = tile / (4 * columns), in_band = tile - band * 4 * columns;
         const unsigned height = (unsigned)tiles.total - 4 * band < 4 ? tiles.total - 4 * band : 4;
@@ -757,7 +757,7 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
     const int r16 = lane & 15, quarter = lane >> 4;
     RowTiles<16> tiles(p);
     unsigned tile;
-    if (!xcd_run(blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
+    if (!xcd_run(p.first_block + blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
     const RowTile at = tiles.find(tile / columns);
     const int n0 = tile % columns * (16 * NT * PARTS);
     const bool nobody = at.expert == p.experts;
@@ -933,7 +933,22 @@ inline long long row_tiles_at_most(const ProductParams& p, int height)
     const long long cut = p.experts + 1 < p.rows ? p.experts + 1 : p.rows;      // groups whose last tile is not full, the rows of no group too
     return p.rows / height + cut;
 }
-constexpr long long kMostBlocks = 0xffffff;       // a grid holds fewer than 2^32 threads
+// Workgroups in as many grids as they need: a grid holds fewer than 2^32 threads, 2^23 workgroups of up to 512 less eight (a multiple of eight, so that
+// the XCDs go on in turn).  Numbers of 32 bits do for every result that memory holds.
+constexpr long long kMostBlocks = 0xffffffffLL, kGridBlocks = (1LL << 23) - 8;
+template <typename Launch>
+hipError_t launch_grids(const ProductParams& p, long long blocks, Launch launch)
+{
+    if (blocks > kMostBlocks) return hipErrorInvalidConfiguration;
+    ProductParams q = p;
+    for (long long first = 0; first < blocks; first += kGridBlocks) {
+        q.first_block = (unsigned)first;
+        launch(q, (unsigned)(blocks - first < kGridBlocks ? blocks - first : kGridBlocks));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 template <int DIRECTION, int TYPE, int BM, int BN, int STAGES, bool ANY, typename Out>
 hipError_t launch_whole_tiles(const ProductParams& p, hipStream_t s)
@@ -942,9 +957,9 @@ hipError_t launch_whole_tiles(const ProductParams& p, hipStream_t s)
     long long blocks;
     if (DIRECTION == kDw) blocks = (columns * ((p.height + BM - 1) / BM) + 7) / 8 * 8 * p.experts;
     else blocks = (row_tiles_at_most(p, BM) * columns + 7) / 8 * 8;
-    if (blocks * p.splits > kMostBlocks) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((product_kernel<DIRECTION, TYPE, BM, BN, 2, 2, STAGES, ANY, Out>), dim3((unsigned)blocks, p.splits), dim3(256), 0, s, p);
-    return hipGetLastError();
+    return launch_grids(p, blocks, [&](const ProductParams& q, unsigned count) {
+        hipLaunchKernelGGL((product_kernel<DIRECTION, TYPE, BM, BN, 2, 2, STAGES, ANY, Out>), dim3(count, p.splits), dim3(256), 0, s, q);
+    });
 }
 
 template <int DIRECTION, int TYPE, int BM, int BN, int STAGES, bool ANY, typename Out>
@@ -971,9 +986,9 @@ hipError_t launch_few_rows(const ProductParams& p, const RawRows& raw, hipStream
     constexpr int width = 16 * NT * (RAW ? 2 : 1);
     const long long columns = (p.width + width - 1) / width;
     const long long blocks = (row_tiles_at_most(p, 16) * columns + 7) / 8 * 8;
-    if (blocks > kMostBlocks) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((few_rows_kernel<TYPE, NT, Out, RAW>), dim3((unsigned)blocks), dim3(RAW ? 512 : 256), 0, s, p, (unsigned)columns, raw);
-    return hipGetLastError();
+    return launch_grids(p, blocks, [&](const ProductParams& q, unsigned count) {
+        hipLaunchKernelGGL((few_rows_kernel<TYPE, NT, Out, RAW>), dim3(count), dim3(RAW ? 512 : 256), 0, s, q, (unsigned)columns, raw);
+    });
 }
 
 // whether every row that a kernel loads in pieces of 16 bytes is made of whole aligned ones, and 256 rows lie within 32 bits
