@@ -226,7 +226,7 @@ __device__ __forceinline__ void load_to_lds(uintx4* to, const char* from, unsign
     const unsigned long long base = reinterpret_cast<unsigned long long>(from);
     const intx4 buffer = {(int)base, (int)(base >> 32) & 0xffff, (int)kFar, 0x00027000};
     const unsigned place = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)to);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(buffer), "s"(place) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(buffer), "s"(place) : "memory", "m0");
 }
 
 // An operand's part of a tile in LDS, SPAN rows (or columns) by a chunk of depth, and its way there.

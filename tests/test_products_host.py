@@ -1,4 +1,8 @@
 """The 4-bit and grouped products on the host: what is refused before anything is launched, and which form of the kernels sizes take."""
+import glob
+import os
+import re
+
 import pytest
 
 from test_abi_host import _NoLaunch
@@ -55,3 +59,16 @@ def test_workspace_sizes_of_what_is_refused_are_none(b):
     assert b.spinner_grouped_matmul_dw_workspace_bytes(4100, 40, FAR + 264, 1) == 0
     assert b.spinner_grouped_matmul_dw_workspace_bytes(4100, 40, 264, FAR + 1) == 0
     assert b.spinner_grouped_matmul_dw_workspace_bytes(4100, 40, 264, 1) > 0
+
+
+def test_inline_assembly_declares_the_m0_that_it_writes():
+    """The compiler keeps values of its own in m0 (spills, indexing): a statement that writes it has to say so."""
+    from paper_1610_06209_amd import build
+
+    found = 0
+    for path in sorted(glob.glob(os.path.join(build.CSRC, "*.h*"))):
+        for statement in re.findall(r"\basm\b[^;]*?\((.*?)\);", open(path).read(), re.S):
+            if re.search(r"\bm0\s*,", statement):
+                found += 1
+                assert re.search(r":[^:]*\"m0\"[^:]*$", statement), (path, statement)
+    assert found
