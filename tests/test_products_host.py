@@ -5,6 +5,7 @@ import re
 
 import pytest
 
+import product_forms as forms
 from test_abi_host import _NoLaunch
 from test_streams_host import T, h, u8
 
@@ -72,3 +73,32 @@ def test_inline_assembly_declares_the_m0_that_it_writes():
                 found += 1
                 assert re.search(r":[^:]*\"m0\"[^:]*$", statement), (path, statement)
     assert found
+
+
+def test_the_rule_for_forms_is_read_aright():
+    """The weight gradient's shares are those that its workspace is made for, by the public call."""
+    from paper_1610_06209_amd import binding
+
+    for rows, experts, k, n in forms.SIXTEEN + [(1, 1, 1, 1), (70000, 7, 40, 56)]:
+        shares = forms.plan(forms.DW, False, rows, experts, k, n)[2]
+        assert binding.spinner_grouped_matmul_dw_workspace_bytes(rows, n, k, experts) == (4 * shares * experts * k * n if shares > 1 else 0)
+    assert forms.plan(forms.FORWARD, False, 16, 1, 512, 512)[0] == forms.plan(forms.FORWARD, True, 64, 32, 512, 512)[0] == "few rows"
+
+
+@pytest.mark.parametrize("one", [True, False])
+@pytest.mark.parametrize("direction", [forms.FORWARD, forms.DX])
+def test_tested_sizes_run_through_each_form(direction, one):
+    """Sizes of test_gpu_product_depth.py: for each form more chunks of depth than its buffers hold, by the library's rule as it stands."""
+    found = {forms.runs_through(direction, False, *s) for s in forms.SIXTEEN if (s[1] == 1) == one} - {None}
+    assert found == {(f, False) for f in forms.STAGES}
+
+
+def test_tested_sizes_run_through_each_form_of_weight_gradients():
+    found = {forms.runs_through(forms.DW, False, *s) for s in forms.SIXTEEN if s[1] == 1} - {None}
+    assert found == {(f, shares) for f in forms.STAGES for shares in (False, True)}
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_tested_sizes_run_through_each_form_in_4_bits(one):
+    found = {forms.runs_through(forms.FORWARD, True, *s) for s in forms.FOUR if (s[1] == 1) == one} - {None}
+    assert found == {(f, False) for f in ("256", "128", "64")}
