@@ -103,3 +103,29 @@ def test_weight_gradients_of_many_columns(gpu):
             assert not bool(dw[e].any()), e
     for e, (lo, hi) in used.items():                       # small whole numbers: sums are exact before the one rounding
         assert t.equal(dw[e, 0], (dy[lo:hi].float() * x[lo:hi].float()).sum(0).bfloat16())
+
+
+def test_layers_beyond_32_bits_give_the_bits_of_their_parts(gpu):
+    """4.4e9 numbers in, 2.2e9 out: the same rows time after time give the same results wherever they lie, and those of the 64-bit definition."""
+    rows, k, n = (1 << 21) + 77, 2080, 1040
+    say("a layer beyond 32 bits", rows, k, n)
+    t, b = gpu.torch, gpu.b
+    t.cuda.empty_cache()
+    gen = t.Generator(device=gpu.dev)
+    gen.manual_seed(1)
+    part = t.randn((1 << 14, k), generator=gen, device=gpu.dev).bfloat16()
+    x = t.empty((rows, k), dtype=t.bfloat16, device=gpu.dev)
+    for r in range(0, rows, 1 << 14):
+        x[r:r + (1 << 14)] = part[: rows - r]
+    wc, ws = b.spinner_mx_quantize(t.randn((n, k), generator=gen, device=gpu.dev), None, 32)
+    y = b.spinner_mx_linear(x, wc, ws, None, 32)
+    for r in range(1 << 14, rows, 1 << 14):
+        assert t.equal(y[r:r + (1 << 14)], y[: min(1 << 14, rows - r)]), r
+    ac, as_ = b.spinner_mx_quantize(part[:200], None, 32)
+    a, w = (mx.values(c.cpu().numpy(), s.cpu().numpy()) for c, s in ((ac, as_), (wc, ws)))
+    want, size = a @ w.T, np.abs(a) @ np.abs(w).T
+    # one rounding to bf16, (k / 64 + 64) additions off by at most 2^-23 of the sum of magnitudes
+    for at in (0, (rows >> 14) << 14):
+        upto = min(200, rows - at)
+        off = np.abs(y[at:at + upto].double().cpu().numpy() - want[:upto])
+        assert np.all(off <= np.abs(want[:upto]) * 1.01 * 2.0 ** -8 + size[:upto] * (k / 64 + 64) * 2.0 ** -23)
