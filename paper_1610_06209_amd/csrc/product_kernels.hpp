@@ -1010,8 +1010,10 @@ template <int TYPE, typename Out, bool RAW>
 hipError_t launch_few_rows_as(const ProductParams& p, const RawRows& raw, hipStream_t s)
 {
     const long long sixteens = (p.width + 15) / 16 * (long long)(p.experts < p.rows ? p.experts : p.rows);
-    if constexpr (RAW) {              // (columns for two groups of waves)
-        if (sixteens >= 4096) return launch_few_rows<TYPE, 2, Out, true>(p, raw, s);
+    if constexpr (RAW) {
+        // (columns for two groups of waves, every workgroup quantises)  16 / 32, in us, bf16: one row, k = 4096, n = 8192 5.85 / 8.1, n = 16384 9.3 / 10.2, 32768 17.2 / 14.2,
+        // 65536 28.4 / 27.0; k = 2048, n = 32768 11.4 / 9.1; four rows, k = 1024, n = 65536 15.3 / 12.3
+        if (sixteens >= 2048) return launch_few_rows<TYPE, 2, Out, true>(p, raw, s);
         return launch_few_rows<TYPE, 1, Out, true>(p, raw, s);
     } else {
         if constexpr (TYPE == kMx4)
