@@ -988,7 +988,7 @@ def spinner_mx_linear_workspace_bytes(rows: int, k: int) -> int:
 def spinner_mx_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, out=None, workspace=None, stream=None):
     """A layer with 4-bit weights on plain inputs: spinner_mx_quantize(x, diag, block), then spinner_mx_matmul; out of the type of x.
 
-    The weights are quantised with the same diag and block, which then cancel in the product.
+    The weights are quantised with the same diag and block, which then cancel in the product.  Results have no autograd history, and there is no gradient of this call.
     """
     r = _native_products.mx_linear(x, w_codes, w_scales, diag, block, ends, out, workspace, stream)
     if r is not None:
@@ -1030,6 +1030,7 @@ def spinner_grouped_matmul(x, w, ends=None, out=None, stream=None):
     """out = x w^T of each expert's rows with its own weights: x bf16 or fp16 [rows][k], w [experts][n][k] (or [n][k] without ends).
 
     ends: int64 CUDA tensor [experts]; the rows of expert e are ends[e - 1] .. ends[e].  Rows from the last end on come out as 0.
+    As everywhere here, results have no autograd history: the gradients are spinner_grouped_matmul_dx and spinner_grouped_matmul_dw.
     """
     r = _native_products.grouped_matmul(x, w, ends, out, stream)
     return r if r is not None else _grouped(lib.spinner_grouped_matmul, x, w, ends, out, stream, True)

@@ -8,11 +8,11 @@ namespace {
 
 // Rows [rows][k] to codes and scales, v = H D x on each run of 2^LOG coordinates first (LOG = 0: v = x).
 // Eight numbers a lane (fp32: four and four, 16 bytes each; eight neighbours, whose two loads take every second piece of a line, 16384 x 16384 254 us;
-// so 214).  Waves of a run longer than a wave's 512 numbers meet in LDS (in registers alone, 64 numbers a lane at 2^12, a wave's 240 registers
+// so 219).  Waves of a run longer than a wave's 512 numbers meet in LDS (in registers alone, 64 numbers a lane at 2^12, a wave's 240 registers
 // left one wave a SIMD: one row of 4096 12.9 us, here 3.5).
 // A wave stays with its columns, whose diagonal it keeps, and goes down the rows, the next row's numbers asked for ahead.
-// Measured, bf16 16384 x 8192 (340 MB): no rotation 58 us, 5.9 TB/s (the copy rate is 6.2), runs of 512 82 us (bound by the vector ALU: 15 instructions
-// a number), 1024 90, 4096 112 (the sums in LDS).
+// Measured, bf16 16384 x 8192 (340 MB): no rotation 57 us, 6.0 TB/s (the copy rate is 6.2), runs of 256 64, 512 73, 1024 82, 2048 92, 4096 105.  Runs are bound by the vector
+// ALU: 15 (256), 17 (512) to 24 (4096) instructions a number keep it busy 82 to 92 % of the time, without a rotation 5 and 30 %.
 template <typename T, int LOG>
 __global__ void __launch_bounds__(LOG > 9 ? 64 * waves_of_run(LOG) : 256) mx4_quantize_kernel(QuantizeParams p, int column_groups, int row_step)
 {
@@ -90,8 +90,8 @@ hipError_t quantize(const QuantizeParams& p, hipStream_t s)
 {
     constexpr int waves = waves_of_run(LOG), width = waves * kChunk;
     const int groups = (p.k + width - 1) / width;
-    // waves enough to fill the chip, no more than rows; each then goes down several rows (runs of 512, bf16 16384 x 8192: 8192 waves 85 us, 16384 82; no
-    // rotation, runs of 1024: the same)
+    // waves enough to fill the chip, no more than rows; each then goes down several rows.  8192 / 16384 waves, bf16, in us: runs of 512, 16384 x 8192 74.0 / 72.8; no
+    // rotation 57.4 / 57.0; runs of 1024 and 4096, 16384 x 8192 82 / 79 and 105 / 101, but 2048 x 4096 6.7 / 7.3 and 8.0 / 8.4
     const int want = ((LOG > 0 && waves == 1 ? 16384 : 8192) / waves + groups - 1) / groups;
     const int row_step = p.rows < want ? p.rows : want;
     const long long units = (long long)groups * row_step, blocks = waves > 1 ? units : (units + 3) / 4;
@@ -148,7 +148,9 @@ struct Form {
 };
 constexpr Form kForms16[] = {{kTile256, 256, 1.1, 1.6, 10, 256}, {kTile128, 128, 0.62, 0.95, 5, 512}, {kTile128Deep, 128, 0.45, 0.5, 5, 256}, {kTile64, 64, 0.22, 0.37, 3.5, 512}};
 constexpr Form kForms4[] = {{kTile256, 256, 1.25, 2.0, 6, 256}, {kTile128, 128, 0.7, 1.15, 4, 512}, {kTile64, 64, 0.33, 0.33, 3, 256}};
-constexpr int kHeldDepth = 8192;                 // 64 x 64 tiles hold the scales of so many 4-bit numbers of a row
+// 64 x 64 tiles hold the scales of so many 4-bit numbers of a row, 33 of 100 KB of LDS; deeper sums take tiles of 128 x 128: 37 x 10007 x 8192 12.7 us, x 8224 33.0; 37 x 4096 x 8192
+// 10.5, x 14336 40.7
+constexpr int kHeldDepth = 8192;
 constexpr size_t kMostPartial = 64u << 20;       // bytes of partial sums
 
 template <int N>
@@ -160,7 +162,8 @@ static void shortest(const Form (&forms)[N], int direction, bool mx4, ProductPar
         double tiles = (p->width + f.side - 1) / f.side, chunks;
         if (direction == kDw) {
             tiles *= (double)((p->height + f.side - 1) / f.side) * p->experts;
-            // the longest group of several, taken as half as long again as they are on average
+            // the longest group of several, taken as half as long again as they are on average, which the host does not know to be so: 8192 rows, 16 experts, k = n = 1024
+            // 28 us where they are equal, 90 with half of the rows in one group, 163 with all; 32768 rows, 8 experts, k = n = 4096 978, 956, 960
             chunks = ceil(p->rows * (p->experts > 1 ? 1.5 : 1.0) / p->experts / 64);
         } else {
             // a group's last tile is half full on average
@@ -185,12 +188,16 @@ static void shortest(const Form (&forms)[N], int direction, bool mx4, ProductPar
     }
 }
 
+// (16-bit rows that are no whole pieces of 16 bytes go by the same choice, though their kernels, 64 x 64 or 128 x 128 and a chunk ahead through registers, take longer: see
+// launch_product_as)
 void plan_product(int direction, bool mx4, ProductParams* p)
 {
     p->splits = 1;
     if (direction == kForward) {
         // up to sixteen rows a group the weights' way from memory is all (4 bits, n = 16384, k = 4096, 16 rows: 9.8 us, 64 x 64 tiles 10.7; 32 rows: 15.2, 10.8);
-        // and tiles read 4-bit operands' scales sixteen at a time
+        // and tiles read 4-bit operands' scales sixteen at a time.  It goes by the mean, as the rows of each group are known on the GPU only.  Few rows / tiles of 128 x 128 in us, bf16 and 4 bits:
+        // 1024 rows, 64 experts, k = 2048, n = 4096, groups of 16 199 / 193 and 65 / 58, all rows in one group 175 / 25 and 57 / 9; 256 rows, 16 experts, k = n = 4096, groups of 16
+        // 134 / 126 and 27 / 23, in one 87 / 42 and 28 / 11
         const long long scales = p->depth / kMx4Block;
         if ((p->rows + p->experts - 1) / p->experts <= 16 || (mx4 && (p->rows * scales < 16 || p->experts * (p->width * scales) < 16))) {
             p->tile = kFewRows;

@@ -358,9 +358,9 @@ constexpr int workgroups_a_unit(int side, int stages, int type) { return side ==
 // SIMD with 256 sums, two chunks in LDS.  That form hides what it waits for in its own order: operands a step ahead of their products, loads straight to
 // LDS a chunk ahead and between the products, one meeting of the waves a chunk, with a step's products still to come.  It takes the numbers of
 // tiles that leave many compute units idle; then smaller ones are ahead (see plan_product).
-// Measured: 16384 x 8192 x 8192 in 4 bits 568 us, 3.9 PFLOP/s; 16384 x 4096 x 4096 154 us, 3.6; bf16 16384 x 4096 x 4096 y 452 us, 1.22 PFLOP/s, dx 433, 1.27,
-// dw 440, 1.25 (the library behind torch, one weight matrix: 402, 1.37).  Bound: half and a little more of the time the matrix pipe is busy, at 1.7 to 2.1 GHz
-// under its load; without the loads the 4-bit product takes 491 us, without the reads of LDS either 449.  In us, 4 bits / bf16: reads of
+// Measured: 16384 x 8192 x 8192 in 4 bits 518 us, 4.2 PFLOP/s; 16384 x 4096 x 4096 138 us, 4.0; bf16 16384 x 4096 x 4096 y 394 to 411 us, 1.34 to 1.39 PFLOP/s, dx 419, 1.31,
+// dw 432, 1.27 (the library behind torch, y with one weight matrix: 337, 1.63).  Bound: half and a little more of the time the matrix pipe is busy, at 1.7 to 2.1 GHz
+// under its load; with neither the loads nor the reads of LDS the 4-bit product takes 425 to 445 us.  In us as the kernel was then, 4 bits / bf16: reads of
 // LDS that the compiler put right before their products 851 / 1068; banks covered eight lanes at a time, all loads of a chunk in one step 798 / 1000;
 // scales straight from memory 763; results stored from registers 595 / 228 a quarter of the rows, through LDS 571 / 223; eight waves of 128 x 64
 // 623 (four 574) / 1030 (980).  Lines touched two to four chunks ahead of their loads, to have them in the L2: 632 / 512.
@@ -1029,7 +1029,8 @@ hipError_t launch_product_as(const ProductParams& p, hipStream_t s)
     if constexpr (DIRECTION == kForward)
         if (p.tile == kFewRows) return launch_few_rows_as<TYPE, Out, false>(p, RawRows{}, s);
     if constexpr (TYPE != kMx4) {
-        // (the same order of the sums as with whole pieces: each number's in the order of the depth, or a quarter of each chunk a wave)
+        // (the same order of the sums as with whole pieces: each number's in the order of the depth, or a quarter of each chunk a wave.)  y, dx, dw in us beside the next sizes of whole
+        // pieces: 16384 x 4095 x 4097 837, 871, 1200 for 411, 419, 432; 20000 x 301 x 403, 16 experts 27, 23, 127 for 17, 12, 45; 24 x 4095 x 2047, 8 experts (y: few rows) 62, 44, 80 for 21, 25, 53
         if (!whole_pieces<DIRECTION, TYPE>(p))
             return p.tile == kTile64 ? launch_tiles<DIRECTION, TYPE, 64, 64, 2, true, Out>(p, s) : launch_tiles<DIRECTION, TYPE, 128, 128, 2, true, Out>(p, s);
         if (p.tile == kTile128Deep) return launch_tiles<DIRECTION, TYPE, 128, 128, 4, false, Out>(p, s);
