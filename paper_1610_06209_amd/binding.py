@@ -217,19 +217,18 @@ def _stream_handle(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
+_new_on = _native._new_on
+
+
 def _new(shape, dtype, device, stream, scratch=False):
     """Memory for a result, or for scratch that is let go of on return, of a call on ``stream``.
 
     With an explicit stream it is memory of that stream: a block that the current stream has let go of may still be read or written by what
     is queued there.  A result is then used on the current stream too.
     """
-    if stream is None or device.type != "cuda":
+    if stream is None or device.type != "cuda" or stream.cuda_stream == _stream_handle(None):
         return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if not scratch:
-        t.record_stream(torch.cuda.current_stream(device))
-    return t
+    return _new_on(shape if isinstance(shape, tuple) else (shape,), dtype, device.index, stream.cuda_stream, scratch)
 
 
 def _check_tensor(t, name, dtype):

@@ -78,6 +78,7 @@ def check_call(g, call, monkeypatch):
     with monkeypatch.context() as m:
         m.setattr(t, "empty", noted(empty))
         m.setattr(t, "empty_like", noted(empty_like))
+        m.setattr(g.b, "_new_on", noted(g.b._new_on))
         got = call(stream=side)
     places = [(m.data_ptr(), m.numel()) for m in made]
     side.synchronize()
@@ -163,3 +164,28 @@ TRANSFORMS = ["apply", "apply_signs", "apply_blocks", "pack_signs", "hash", "has
 def test_transforms_on_a_stream_of_their_own(gpu, name, monkeypatch):
     say("stream of its own", name)
     check_call(gpu, transform_calls(gpu)[name], monkeypatch)
+
+
+def test_whatever_has_a_handle_is_a_stream(gpu):
+    """A stream object that has the handle alone, the default stream while another one is current, and the current one itself."""
+    say("streams by their handle")
+    t, b = gpu.torch, gpu.b
+    x, w = t.randn((40, 512), device=gpu.dev).bfloat16(), t.randn((64, 512), device=gpu.dev).bfloat16()
+    want = b.spinner_grouped_matmul(x, w)
+    t.cuda.synchronize()
+    side = t.cuda.Stream()
+    owner = lambda r: [s["stream"] for s in t.cuda.memory_snapshot() if s["address"] <= r.data_ptr() < s["address"] + s["total_size"]]          # noqa: E731
+    r = b.spinner_grouped_matmul(x, w, stream=type("Handle", (), {"cuda_stream": side.cuda_stream})())
+    side.synchronize()
+    assert t.equal(r, want) and owner(r) == [side.cuda_stream]
+    with t.cuda.stream(side):
+        r = b.spinner_grouped_matmul(x, w, stream=t.cuda.default_stream())
+        assert t.cuda.current_stream() == side
+        t.cuda.default_stream().synchronize()
+        assert t.equal(r, want) and owner(r) == [0]
+        r = b.spinner_grouped_matmul(x, w, stream=side)
+        assert t.equal(r, want) and owner(r) == [side.cuda_stream]
+    t.cuda.synchronize()
+    with pytest.raises(t.cuda.OutOfMemoryError):                     # refused memory is an error, and leaves the current stream as it was
+        b._new_on((1 << 50,), t.uint8, 0, side.cuda_stream, False)
+    assert t.cuda.current_stream() == t.cuda.default_stream()

@@ -1,7 +1,5 @@
 """Where the memory comes from that a call makes for itself when it is given a stream: from that stream, whatever the current one has queued
 on blocks that it let go of.  On the host, with tensors that are only described and a library that launches nothing."""
-import contextlib
-
 import pytest
 
 from test_abi_host import _NoLaunch, _Tensor
@@ -29,31 +27,31 @@ class _OnGpu(_Tensor):
 
 @pytest.fixture
 def made(monkeypatch):
-    """Every tensor that is made, with the stream that was current then; the binding without launches."""
+    """Every tensor that is made, with the stream whose memory it is; the binding without launches."""
     import torch
 
     from paper_1610_06209_amd import binding as b
 
-    tensors, streams = [], [CURRENT]
+    tensors = []
 
     def empty(*shape, dtype=torch.float32, device=None):
         shape = shape[0] if len(shape) == 1 and not isinstance(shape[0], int) else shape
-        tensors.append(_OnGpu(*shape, dtype=str(dtype)[6:], made_on=streams[-1]))
+        tensors.append(_OnGpu(*shape, dtype=str(dtype)[6:], made_on=CURRENT))
         return tensors[-1]
 
-    @contextlib.contextmanager
-    def on(stream):
-        streams.append(stream)
-        yield
-        streams.pop()
+    def new_on(shape, dtype, device, handle, scratch):
+        assert device == 0 and handle == MINE.cuda_stream
+        t = empty(shape, dtype=dtype)
+        t.made_on = MINE
+        if not scratch:
+            t.record_stream(CURRENT)
+        return t
 
     monkeypatch.setattr(torch, "empty", empty)
-    monkeypatch.setattr(torch, "empty_like", lambda t: empty(*t.shape, dtype=t.dtype))
-    monkeypatch.setattr(torch.cuda, "stream", on)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda *device: streams[-1])
+    monkeypatch.setattr(b, "_new_on", new_on)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(b, "lib", _NoLaunch(b.lib))
-    monkeypatch.setattr(b, "_stream_handle", lambda stream: (stream or streams[-1]).cuda_stream)
+    monkeypatch.setattr(b, "_stream_handle", lambda stream: (stream or CURRENT).cuda_stream)
     return b, tensors
 
 
@@ -111,4 +109,11 @@ def test_memory_comes_from_the_stream_of_the_call(made, name):
 def test_memory_of_other_calls_comes_from_the_current_stream(made, name):
     b, tensors = made
     getattr(b, name)(**CALLS[name])
+    assert tensors and all(t.made_on is CURRENT and not t.used_on for t in tensors)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_the_current_stream_given_is_the_current_stream(made, name):
+    b, tensors = made
+    getattr(b, name)(stream=type("Stream", (), {"cuda_stream": CURRENT.cuda_stream})(), **CALLS[name])
     assert tensors and all(t.made_on is CURRENT and not t.used_on for t in tensors)
