@@ -137,3 +137,32 @@ def test_layers_of_few_rows_with_many_columns(gpu, name, rows, experts, k, n, bl
     w = w.view(experts, n, k)
     for i, (lo, hi) in enumerate(mx.bounds(ends.cpu().numpy(), experts, rows)):
         check(got[lo:hi], a[lo:hi] @ w[i].T, a[lo:hi].abs() @ w[i].abs().T, (k / 64 + 64) * 2.0 ** -23, name)
+
+
+@pytest.mark.parametrize("rows,experts,k,n", [(3, 1, 1056, 65), (19, 1, 2656, 37), (57, 3, 2784, 32), (113, 3, 1152, 5237), (2050, 1, 1056, 4104), (300, 64, 544, 1030)])
+def test_scales_of_any_alignment(gpu, rows, experts, k, n):
+    """Scales that start anywhere, at the beginning and at the end of their memory: the bits of aligned ones, from every form."""
+    say("scales of any alignment", rows, experts, k, n, forms.plan(0, True, rows, experts, k, n))
+    t, b = gpu.torch, gpu.b
+    gen = t.Generator(device=gpu.dev)
+    gen.manual_seed(rows + n)
+    codes = lambda r: t.randint(0, 256, (r, k // 2), generator=gen, device=gpu.dev, dtype=t.uint8)          # noqa: E731
+    scales = lambda r: t.randint(112, 122, (r, k // 32), generator=gen, device=gpu.dev, dtype=t.uint8)      # noqa: E731
+
+    def moved(s, by):
+        flat = t.full((s.numel() + by,), 255, device=gpu.dev, dtype=t.uint8)
+        flat[by:] = s.flatten()
+        return flat[by:].view(s.shape)
+
+    ac, as_, wc, ws = codes(rows), scales(rows), codes(experts * n).view(experts, n, -1), scales(experts * n).view(experts, n, -1)
+    ends = t.from_numpy(ragged(np.random.default_rng(rows), rows, experts, 1)).to(gpu.dev)
+    want = b.spinner_mx_matmul(ac, as_, wc, ws, ends, t.float32)
+    back = b.spinner_mx_dequantize(ac, as_)
+    x = t.randn((rows, k), generator=gen, device=gpu.dev).bfloat16()
+    quantised = b.spinner_mx_quantize(x, None, 32)
+    for by in (1, 3, 8, 13):
+        assert t.equal(b.spinner_mx_matmul(ac, moved(as_, by), wc, moved(ws, 16 - by), ends, t.float32), want)
+        assert t.equal(b.spinner_mx_dequantize(ac, moved(as_, by)), back)
+        got = b.spinner_mx_quantize(x, None, 32, scales=moved(as_, by))
+        assert t.equal(got[0], quantised[0]) and t.equal(got[1], quantised[1])
+        assert t.equal(b.spinner_mx_linear(x, wc, moved(ws, by), None, 32, ends), b.spinner_mx_linear(x, wc, ws, None, 32, ends))
