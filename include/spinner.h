@@ -502,6 +502,153 @@ int spinner_grouped_matmul_dw(const void *dy, const void *x, int dtype, long row
 size_t spinner_grouped_matmul_dw_workspace_bytes(long rows, int n, int k, int experts);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Layers of 8-bit whole numbers
+ * ---------------------------------------------------------------------------
+ * Between the trained 16 bits and the 4 bits above: a row (a token's vector, or
+ * an output channel's weights) is whole numbers of 8 bits and one fp32 scale.
+ * codes is int8 [rows][width], width = k rounded up to a multiple of 16, zeros
+ * behind the k numbers; scales is fp32 [rows].  Sums of products are exact (32
+ * bits), rounded to fp32 once and multiplied by the scales of w and of a.
+ */
+
+/*
+ * Rotate and quantise.  v = H D x on runs of `block` coordinates as in
+ * spinner_mx_quantize (block = 0: v = x, any k).  Scale a / 127, a = max |v| of
+ * the row, rounded to fp32 and held at 2^-126 and above; codes v / scale rounded
+ * to the nearest, ties to even (with a rotation: of v as fp32 butterflies leave
+ * it, to within 2e-5 of a tie).  A NaN or an infinity in a row: scale NaN,
+ * codes 0, so that every product with the row is NaN.
+ *
+ *   x         in   device [rows][k] of type dtype, rows x_stride >= 0 elements apart
+ *   k         in   1 <= k <= 2^17 - 16; a multiple of block
+ *   places    in   device int32 [rows][top] or NULL (top = 1).  The codes and the
+ *                  scale of row r go to each of the places in its row of `places`
+ *                  (see spinner_route_order) of [rows * top]; NULL: to place r.
+ *                  Places outside [0, rows * top) are passed over.
+ *   top       in   1 <= top <= 32, rows * top <= 2^31 - 2^16
+ *   codes     out  device int8 [rows * top][width]
+ *   scales    out  device fp32 [rows * top]
+ */
+int spinner_int_quantize(const void *x, int dtype, long rows, int k, long x_stride,
+                         const float *diag, int block, const int *places, int top,
+                         void *codes, float *scales, void *stream);
+
+/* The numbers that codes stand for, to out [rows][k] of type dtype, rows out_stride >= k elements apart. */
+int spinner_int_dequantize(const void *codes, const float *scales, long rows, int k,
+                           void *out, int dtype, long out_stride, void *stream);
+
+/*
+ * out[r][j] = sum_i a[r][i] w[e][j][i] with a [rows][k] and w [experts][n][k] in
+ * the format above; groups, ends, rows of no expert and out as in
+ * spinner_mx_matmul.  k <= 2^17 - 16 keeps the sums in 32 bits, whatever the codes.
+ */
+int spinner_int_matmul(const void *a_codes, const float *a_scales, long rows, int k,
+                       const void *w_codes, const float *w_scales, int n,
+                       int experts, const long long *ends,
+                       void *out, int dtype, long out_stride, void *stream);
+
+/*
+ * spinner_int_quantize and spinner_int_matmul in one call, out [rows * top][n] of
+ * the type of x.  With places it is a routed layer's way in: each row is rotated
+ * and rounded once and goes to its experts in 8 bits; every place has to be named
+ * once, as spinner_route_order does (a place that is not has undefined results).
+ * workspace: spinner_int_linear_workspace_bytes(rows * top, k) bytes; NULL will do
+ * without places for up to eight runs of 512 numbers, as in spinner_mx_linear.
+ */
+size_t spinner_int_linear_workspace_bytes(long rows, int k);
+int spinner_int_linear(const void *x, int dtype, long rows, int k, long x_stride,
+                       const float *diag, int block, const int *places, int top,
+                       const void *w_codes, const float *w_scales, int n,
+                       int experts, const long long *ends,
+                       void *out, long out_stride, void *workspace, void *stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Routing: from a router's logits to the experts' rows, and back
+ * ---------------------------------------------------------------------------
+ */
+enum { SPINNER_SCORE_SOFTMAX = 0, SPINNER_SCORE_SIGMOID = 1 };
+
+/*
+ * For every row the `top` experts of the largest keys, largest first, ties to the
+ * lowest index, and their weights.  With s the scores (softmax over the row or
+ * sigmoid of each logit) the keys are s + bias, or, without a bias, the logits,
+ * which order experts as the scores do; keys that decide are compared as fp64
+ * gives them.  Weights are scale * s, or scale * s / (sum of the chosen s).
+ *
+ *   logits      in   device [rows][experts] of type dtype, stride >= 0 elements apart
+ *   experts     in   1 <= experts <= 1024
+ *   bias        in   device fp32 [experts], added for the choice only, or NULL
+ *   mask        in   device bytes [rows], 0: the row is not routed; or NULL
+ *   score       in   SPINNER_SCORE_SOFTMAX or SPINNER_SCORE_SIGMOID
+ *   groups      in   1 <= groups <= 64, divides experts: runs of experts / groups.
+ *                    Only the top_groups groups of the largest keys take part; a
+ *                    group's key is the largest key in it (group_top = 1) or the
+ *                    sum of the two largest s + bias (group_top = 2).
+ *   top         in   1 <= top <= 32, top <= top_groups * (experts / groups)
+ *   weights     out  device fp32 [rows][top]
+ *   chosen      out  device int32 [rows][top]
+ *
+ * A logit or bias of -inf takes its expert out.  Where fewer experts than `top`
+ * are left, and in rows of mask 0, the rest is expert -1 with weight 0.  A NaN
+ * among the logits and biases of a row (with softmax also a logit of +inf):
+ * expert -1, weight NaN for all of the row.
+ */
+int spinner_route(const void *logits, int dtype, long rows, int experts, long stride,
+                  const float *bias, const void *mask, int score, int groups, int top_groups,
+                  int group_top, int top, int renormalise, float scale,
+                  float *weights, int *chosen, void *stream);
+
+/*
+ * Gradient of the weights with respect to the logits, for the experts as
+ * chosen: dlogits [rows][experts] of type dtype, rows dlogits_stride >= experts
+ * elements apart, all of it written.  Choices outside [0, experts) have none.
+ */
+int spinner_route_grad(const float *dweights, const void *logits, int dtype, long rows, int experts, long stride,
+                       const int *chosen, int score, int top, int renormalise, float scale,
+                       void *dlogits, long dlogits_stride, void *stream);
+
+/*
+ * The order of the experts: place of each of `count` choices (row by row as
+ * spinner_route gives them) when they are sorted by expert, those of one expert
+ * as they come, and where each expert's places end (the `ends` of the products).
+ * Choices outside [0, experts) have their places behind the last end, so that
+ * every place in [0, count) is named once.
+ *
+ *   chosen    in   device int32 [count], 0 <= count <= 2^31 - 2^16
+ *   places    out  device int32 [count]
+ *   ends      out  device int64 [experts]
+ *   workspace      spinner_route_order_workspace_bytes(count, experts) bytes, NULL when that is 0
+ */
+size_t spinner_route_order_workspace_bytes(long count, int experts);
+int spinner_route_order(const int *chosen, long count, int experts, int *places, long long *ends,
+                        void *workspace, void *stream);
+
+/*
+ * Rows to their places, and weighted sums of rows at their places:
+ *     spinner_dispatch      out[places[r][j]] = x[r]
+ *     spinner_combine       out[r] = sum_j weights[r][j] y[places[r][j]]     (weights NULL: ones)
+ *     spinner_combine_grad  dy[places[r][j]] = weights[r][j] dout[r],
+ *                           dweights[r][j] = sum_i dout[r][i] y[places[r][j]][i]
+ * The gradient of spinner_dispatch is spinner_combine without weights.  x, out of
+ * combine and dout are [rows][n], the others [rows * top][n], all of type dtype;
+ * weights and dweights fp32 [rows][top].  Sums are fp32 and j (i) in a fixed order.
+ * Places outside [0, rows * top) are passed over (their dweights are 0); a row of
+ * dispatch's out or of dy that no place names is left as it was, one that several
+ * name is one of theirs.  In spinner_combine what has the weight 0 adds nothing,
+ * whatever its row holds.  1 <= n <= 2^24, 1 <= top <= 32, rows * top <= 2^31 - 2^16,
+ * strides >= 0 (results: >= n) elements.
+ */
+int spinner_dispatch(const void *x, int dtype, long rows, int n, long x_stride, const int *places, int top,
+                     void *out, long out_stride, void *stream);
+int spinner_combine(const void *y, int dtype, long rows, int n, long y_stride, const int *places, const float *weights, int top,
+                    void *out, long out_stride, void *stream);
+int spinner_combine_grad(const void *dout, const void *y, int dtype, long rows, int n, long dout_stride, long y_stride,
+                         const int *places, const float *weights, int top,
+                         void *dy, long dy_stride, float *dweights, void *stream);
+
+/*
  * Bytes of device scratch spinner_apply needs for these arguments: 0 up to the
  * fused limit, and above it when m == n with epilogue NONE; otherwise batch * n * 4.
  * Returns 0 for invalid arguments (spinner_apply reports those).

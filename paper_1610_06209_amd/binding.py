@@ -45,7 +45,10 @@ EXPORTS = ["spinner_apply", "spinner_hash", "spinner_workspace_bytes", "spinner_
            "spinner_struct_workspace_bytes", "spinner_struct_apply_ws",
            "spinner_mx_quantize", "spinner_mx_dequantize", "spinner_mx_matmul", "spinner_mx_linear_workspace_bytes",
            "spinner_mx_linear", "spinner_grouped_matmul", "spinner_grouped_matmul_dx", "spinner_grouped_matmul_dw",
-           "spinner_grouped_matmul_dw_workspace_bytes"]
+           "spinner_grouped_matmul_dw_workspace_bytes",
+           "spinner_int_quantize", "spinner_int_dequantize", "spinner_int_matmul", "spinner_int_linear_workspace_bytes", "spinner_int_linear",
+           "spinner_route", "spinner_route_grad", "spinner_route_order", "spinner_route_order_workspace_bytes",
+           "spinner_dispatch", "spinner_combine", "spinner_combine_grad"]
 
 if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_native.so")):
     raise ImportError(
@@ -162,6 +165,31 @@ lib.spinner_grouped_matmul_dw.restype = _int
 lib.spinner_grouped_matmul_dw.argtypes = [_vp, _vp, _int, _long, _int, _int, _long, _long, _int, _vp, _vp, _int, _vp, _vp]
 lib.spinner_grouped_matmul_dw_workspace_bytes.restype = ctypes.c_size_t
 lib.spinner_grouped_matmul_dw_workspace_bytes.argtypes = [_long, _int, _int, _int]
+_float = ctypes.c_float
+lib.spinner_int_quantize.restype = _int
+lib.spinner_int_quantize.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _vp, _int, _vp, _vp, _vp]
+lib.spinner_int_dequantize.restype = _int
+lib.spinner_int_dequantize.argtypes = [_vp, _vp, _long, _int, _vp, _int, _long, _vp]
+lib.spinner_int_matmul.restype = _int
+lib.spinner_int_matmul.argtypes = [_vp, _vp, _long, _int, _vp, _vp, _int, _int, _vp, _vp, _int, _long, _vp]
+lib.spinner_int_linear_workspace_bytes.restype = ctypes.c_size_t
+lib.spinner_int_linear_workspace_bytes.argtypes = [_long, _int]
+lib.spinner_int_linear.restype = _int
+lib.spinner_int_linear.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _vp, _int, _vp, _vp, _int, _int, _vp, _vp, _long, _vp, _vp]
+lib.spinner_route.restype = _int
+lib.spinner_route.argtypes = [_vp, _int, _long, _int, _long, _vp, _vp, _int, _int, _int, _int, _int, _int, _float, _vp, _vp, _vp]
+lib.spinner_route_grad.restype = _int
+lib.spinner_route_grad.argtypes = [_vp, _vp, _int, _long, _int, _long, _vp, _int, _int, _int, _float, _vp, _long, _vp]
+lib.spinner_route_order_workspace_bytes.restype = ctypes.c_size_t
+lib.spinner_route_order_workspace_bytes.argtypes = [_long, _int]
+lib.spinner_route_order.restype = _int
+lib.spinner_route_order.argtypes = [_vp, _long, _int, _vp, _vp, _vp, _vp]
+lib.spinner_dispatch.restype = _int
+lib.spinner_dispatch.argtypes = [_vp, _int, _long, _int, _long, _vp, _int, _vp, _long, _vp]
+lib.spinner_combine.restype = _int
+lib.spinner_combine.argtypes = [_vp, _int, _long, _int, _long, _vp, _vp, _int, _vp, _long, _vp]
+lib.spinner_combine_grad.restype = _int
+lib.spinner_combine_grad.argtypes = [_vp, _vp, _int, _long, _int, _long, _long, _vp, _vp, _int, _vp, _long, _vp, _vp]
 STRUCT_KINDS = {"circulant": 0, "skew_circulant": 1, "toeplitz": 2, "hankel": 3}
 
 
@@ -1074,3 +1102,318 @@ def spinner_grouped_matmul_dw(dy, x, ends=None, dtype=torch.float32, dw=None, wo
     _done(lib.spinner_grouped_matmul_dw(dy.data_ptr(), x.data_ptr(), code, rows, n, k, dy_stride, x_stride, experts, e, dw.data_ptr(), dw_code,
                                         workspace.data_ptr() if workspace is not None else None, _stream_handle(stream)))
     return dw
+
+
+# ------------------------------------------------------------------ layers of 8-bit whole numbers
+_native_experts = _native._experts
+INT_PIECE = 16
+
+
+def _int_width(k):
+    """Codes of a row of k numbers: whole pieces of 16."""
+    return -(-k // INT_PIECE) * INT_PIECE
+
+
+def _check_codes(t, name, rows=None):
+    """Contiguous int8 rows of whole pieces; returns their width."""
+    _check_here(t, name, torch.int8)
+    if not t.is_contiguous() or t.dim() < 2 or t.shape[-1] % INT_PIECE or (rows is not None and tuple(t.shape[:-1]) != tuple(rows)):
+        raise ValueError("%s must be contiguous rows of a multiple of %d codes%s" % (name, INT_PIECE, "" if rows is None else ", %s of them" % (tuple(rows),)))
+    return t.shape[-1]
+
+
+def _check_floats(t, name, shape):
+    _check_here(t, name, torch.float32)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous, of shape %s" % (name, tuple(shape)))
+
+
+def _check_places(places, rows):
+    """[rows][top]; returns the address and top."""
+    if places is None:
+        return None, 1
+    _check_here(places, "places", torch.int32, 2)
+    if places.shape[0] != rows or not places.is_contiguous():
+        raise ValueError("places must be contiguous, with as many rows as there are")
+    _check_sizes(places.shape[1])
+    return places.data_ptr(), places.shape[1]
+
+
+def spinner_int_quantize(x, diag=None, block=0, places=None, codes=None, scales=None, stream=None):
+    """Rotate runs of ``block`` coordinates (as spinner_mx_quantize does) and round each row to 8-bit whole numbers with one scale.
+
+    x: fp32, bf16 or fp16 CUDA tensor [rows][k], rows any distance apart.  places: int32 [rows][top] as spinner_route_order gives
+    them, or None; each row's codes then go to its places.  Returns (codes int8 [rows * top][k rounded up to 16s], zeros behind the
+    numbers; scales fp32 [rows * top]); see include/spinner.h for the rounding.
+    """
+    r = _native_experts.int_quantize(x, diag, block, places, codes, scales, stream)
+    if r is not None:
+        return r
+    stride = _check_rows(x, "x")
+    rows, k = x.shape
+    _check_sizes(k, int(block))
+    code = _dtype_code(x.dtype)
+    p, top = _check_places(places, rows)
+    slots, width = rows * top, _int_width(k)
+    if codes is None:
+        codes = _new((slots, width), torch.int8, x.device, stream)
+    if scales is None:
+        scales = _new((slots,), torch.float32, x.device, stream)
+    if _check_codes(codes, "codes", (slots,)) != width:
+        raise ValueError("codes must have rows of %d" % width)
+    _check_floats(scales, "scales", (slots,))
+    d = _check_rotation(diag, block, k)
+    _done(lib.spinner_int_quantize(x.data_ptr(), code, rows, k, stride, d, int(block), p, top, codes.data_ptr(), scales.data_ptr(), _stream_handle(stream)))
+    return codes, scales
+
+
+def spinner_int_dequantize(codes, scales, dtype=torch.float32, k=None, out=None, stream=None):
+    """The numbers that 8-bit codes stand for: the first k of every row (all when None), [rows][k] of ``dtype``."""
+    r = _native_experts.int_dequantize(codes, scales, dtype, k, out, stream)
+    if r is not None:
+        return r
+    _check_here(codes, "codes", torch.int8, 2)
+    width = _check_codes(codes, "codes")
+    rows, k = codes.shape[0], width if k is None else int(k)
+    _check_sizes(k)
+    if _int_width(k) != width:
+        raise ValueError("codes of %d numbers have rows of %d" % (k, _int_width(k)))
+    _check_floats(scales, "scales", (rows,))
+    code = _dtype_code(dtype)
+    out, stride = _new_or_checked(out, "out", (rows, k), dtype, codes, stream)
+    _done(lib.spinner_int_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, out.data_ptr(), code, stride, _stream_handle(stream)))
+    return out
+
+
+def _check_int_weights(w_codes, w_scales, width):
+    """[n][width] or [experts][n][width] and a scale for each row; returns experts and n."""
+    experts, n, w = _check_weights(w_codes, "w_codes")
+    _check_sizes(experts, n, w)
+    if _check_codes(w_codes, "w_codes") != width:
+        raise ValueError("w_codes must have rows of %d" % width)
+    _check_floats(w_scales, "w_scales", w_codes.shape[:-1])
+    return experts, n
+
+
+def spinner_int_matmul(a_codes, a_scales, w_codes, w_scales, ends=None, dtype=torch.bfloat16, out=None, stream=None):
+    """out = a w^T on 8-bit operands: a [rows][k], w [n][k], or [experts][n][k] with each expert's rows up to its entry of ``ends``.
+
+    codes and scales as spinner_int_quantize gives them (w's with the experts in front); ends: int64 CUDA tensor [experts],
+    cumulative.  Rows from the last end on come out as 0.
+    """
+    r = _native_experts.int_matmul(a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream)
+    if r is not None:
+        return r
+    _check_here(a_codes, "a_codes", torch.int8, 2)
+    rows, width = a_codes.shape[0], _check_codes(a_codes, "a_codes")
+    _check_sizes(width)
+    _check_floats(a_scales, "a_scales", (rows,))
+    experts, n = _check_int_weights(w_codes, w_scales, width)
+    e = _check_ends(ends, experts, "w_codes")
+    code = _dtype_code(dtype)
+    out, stride = _new_or_checked(out, "out", (rows, n), dtype, a_codes, stream)
+    _done(lib.spinner_int_matmul(a_codes.data_ptr(), a_scales.data_ptr(), rows, width, w_codes.data_ptr(), w_scales.data_ptr(), n, experts, e,
+                                 out.data_ptr(), code, stride, _stream_handle(stream)))
+    return out
+
+
+def spinner_int_linear_workspace_bytes(rows: int, k: int) -> int:
+    return int(lib.spinner_int_linear_workspace_bytes(int(rows), int(k))) if _fits(int(k)) else 0
+
+
+def spinner_int_linear(x, w_codes, w_scales, diag=None, block=0, ends=None, places=None, out=None, workspace=None, stream=None):
+    """A layer with 8-bit weights on plain inputs: spinner_int_quantize(x, diag, block, places), then spinner_int_matmul; out of the type of x.
+
+    The weights are quantised with the same diag and block, which then cancel in the product.  With places (int32 [rows][top]) out has
+    rows * top rows, in the order of the experts.  Results have no autograd history, and there is no gradient of this call.
+    """
+    r = _native_experts.int_linear(x, w_codes, w_scales, diag, block, ends, places, out, workspace, stream)
+    if r is not None:
+        return r
+    x_stride = _check_rows(x, "x")
+    code = _dtype_code(x.dtype)
+    rows, k = x.shape
+    _check_sizes(k, int(block))
+    p, top = _check_places(places, rows)
+    experts, n = _check_int_weights(w_codes, w_scales, _int_width(k))
+    d = _check_rotation(diag, block, k)
+    e = _check_ends(ends, experts, "w_codes")
+    out, stride = _new_or_checked(out, "out", (rows * top, n), x.dtype, x, stream)
+    need = spinner_int_linear_workspace_bytes(rows * top, k)
+    if workspace is None:
+        workspace = _new(need, torch.uint8, x.device, stream, scratch=True)
+    _check_workspace(workspace, need)
+    _done(lib.spinner_int_linear(x.data_ptr(), code, rows, k, x_stride, d, int(block), p, top, w_codes.data_ptr(), w_scales.data_ptr(), n, experts, e,
+                                 out.data_ptr(), stride, workspace.data_ptr(), _stream_handle(stream)))
+    return out
+
+
+# ------------------------------------------------------------------ routing
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _score(score):
+    return SCORES[score] if isinstance(score, str) else int(score)
+
+
+def spinner_route(logits, top, bias=None, mask=None, score="softmax", groups=1, top_groups=1, group_top=1, renormalise=True, scale=1.0, weights=None,
+                  experts=None, stream=None):
+    """The ``top`` experts of each row of logits and their weights: (weights fp32, experts int32), both [rows][top], largest key first.
+
+    logits: fp32, bf16 or fp16 CUDA tensor [rows][experts], rows any distance apart.  The key of an expert is its score (softmax over
+    the row, or "sigmoid") and, for the choice alone, bias (fp32 [experts]); equal keys go by index.  groups > 1: only experts of
+    the top_groups runs of len / groups experts whose largest key (group_top = 2: sum of the two largest) is largest.  weights are
+    scale times the scores, divided by the sum of the chosen ones where ``renormalise``.  Rows whose entry of mask (bool [rows]) is
+    false, and what a row cannot choose (logits of -inf), have expert -1 and weight 0; rows with a NaN expert -1 and weights NaN.
+    """
+    r = _native_experts.route(logits, top, bias, mask, score, groups, top_groups, group_top, renormalise, scale, weights, experts, stream)
+    if r is not None:
+        return r
+    stride = _check_rows(logits, "logits")
+    rows, count = logits.shape
+    code = _dtype_code(logits.dtype)
+    _check_sizes(count, int(top), int(groups), int(top_groups), int(group_top))
+    if bias is not None:
+        _check_floats(bias, "bias", (count,))
+    if mask is not None:
+        _check_here(mask, "mask", None, 1)
+        if mask.dtype not in (torch.bool, torch.uint8) or mask.numel() != rows or not mask.is_contiguous():
+            raise ValueError("mask must be contiguous, one truth value a row")
+    if int(top) < 1:
+        raise SpinnerError(SPINNER_ERR_BAD_SHAPE)
+    if weights is None:
+        weights = _new((rows, int(top)), torch.float32, logits.device, stream)
+    if experts is None:
+        experts = _new((rows, int(top)), torch.int32, logits.device, stream)
+    _check_floats(weights, "weights", (rows, int(top)))
+    _check_here(experts, "experts", torch.int32, 2)
+    if tuple(experts.shape) != (rows, int(top)) or not experts.is_contiguous():
+        raise ValueError("experts has the wrong size")
+    _done(lib.spinner_route(logits.data_ptr(), code, rows, count, stride, None if bias is None else bias.data_ptr(), None if mask is None else mask.data_ptr(),
+                            _score(score), int(groups), int(top_groups), int(group_top), int(top), int(bool(renormalise)), float(scale), weights.data_ptr(),
+                            experts.data_ptr(), _stream_handle(stream)))
+    return weights, experts
+
+
+def spinner_route_grad(dweights, logits, experts, score="softmax", renormalise=True, scale=1.0, dlogits=None, stream=None):
+    """Gradient of spinner_route's weights with respect to the logits, for the experts it chose; of the type of the logits."""
+    r = _native_experts.route_grad(dweights, logits, experts, score, renormalise, scale, dlogits, stream)
+    if r is not None:
+        return r
+    stride = _check_rows(logits, "logits")
+    rows, count = logits.shape
+    code = _dtype_code(logits.dtype)
+    _check_here(experts, "experts", torch.int32, 2)
+    if experts.shape[0] != rows or not experts.is_contiguous():
+        raise ValueError("experts must be contiguous, with as many rows as the logits")
+    top = experts.shape[1]
+    _check_sizes(count, top)
+    _check_floats(dweights, "dweights", (rows, top))
+    dlogits, out_stride = _new_or_checked(dlogits, "dlogits", (rows, count), logits.dtype, logits, stream)
+    _done(lib.spinner_route_grad(dweights.data_ptr(), logits.data_ptr(), code, rows, count, stride, experts.data_ptr(), _score(score), top,
+                                 int(bool(renormalise)), float(scale), dlogits.data_ptr(), out_stride, _stream_handle(stream)))
+    return dlogits
+
+
+def spinner_route_order_workspace_bytes(count: int, experts: int) -> int:
+    return int(lib.spinner_route_order_workspace_bytes(int(count), int(experts))) if _fits(int(experts)) else 0
+
+
+def spinner_route_order(experts, count, places=None, ends=None, workspace=None, stream=None):
+    """Places of choices (int32 [rows][top], as spinner_route gives them) in the order of the ``count`` experts, and where each expert's end.
+
+    Returns (places int32 [rows][top], ends int64 [count]).  Choices of one expert keep their order; those outside [0, count) are
+    placed behind the last end.
+    """
+    r = _native_experts.route_order(experts, count, places, ends, workspace, stream)
+    if r is not None:
+        return r
+    _check_here(experts, "experts", torch.int32, 2)
+    if not experts.is_contiguous():
+        raise ValueError("experts must be contiguous")
+    _check_sizes(int(count))
+    if int(count) < 1:
+        raise SpinnerError(SPINNER_ERR_BAD_SHAPE)
+    if places is None:
+        places = _new(tuple(experts.shape), torch.int32, experts.device, stream)
+    if ends is None:
+        ends = _new((int(count),), torch.int64, experts.device, stream)
+    _check_here(places, "places", torch.int32, 2)
+    if tuple(places.shape) != tuple(experts.shape) or not places.is_contiguous():
+        raise ValueError("places has the wrong size")
+    _check_ends(ends, int(count), "ends")
+    need = spinner_route_order_workspace_bytes(experts.numel(), int(count))
+    if need and workspace is None:
+        workspace = _new(need, torch.uint8, experts.device, stream, scratch=True)
+    _check_workspace(workspace, need)
+    _done(lib.spinner_route_order(experts.data_ptr(), experts.numel(), int(count), places.data_ptr(), ends.data_ptr(),
+                                  workspace.data_ptr() if workspace is not None else None, _stream_handle(stream)))
+    return places, ends
+
+
+def _check_slots(places, name):
+    """Rows and top of places."""
+    _check_here(places, name, torch.int32, 2)
+    if not places.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    _check_sizes(places.shape[1])
+    return tuple(places.shape)
+
+
+def spinner_dispatch(x, places, out=None, stream=None):
+    """Rows to their places: out[places[r][j]] = x[r], out [rows * top][n] of the type of x.  The gradient is spinner_combine without weights."""
+    r = _native_experts.dispatch(x, places, out, stream)
+    if r is not None:
+        return r
+    stride = _check_rows(x, "x")
+    code = _dtype_code(x.dtype)
+    rows, top = _check_slots(places, "places")
+    if x.shape[0] != rows:
+        raise ValueError("places must have as many rows as x")
+    _check_sizes(x.shape[1])
+    out, out_stride = _new_or_checked(out, "out", (rows * top, x.shape[1]), x.dtype, x, stream)
+    _done(lib.spinner_dispatch(x.data_ptr(), code, rows, x.shape[1], stride, places.data_ptr(), top, out.data_ptr(), out_stride, _stream_handle(stream)))
+    return out
+
+
+def spinner_combine(y, places, weights=None, out=None, stream=None):
+    """Weighted sums of rows at their places: out[r] = sum_j weights[r][j] y[places[r][j]], of the type of y (weights fp32 [rows][top], or None: ones).
+
+    Sums are fp32.  What has the weight 0 adds nothing, whatever its row holds.  Results have no autograd history: the gradient is spinner_combine_grad.
+    """
+    r = _native_experts.combine(y, places, weights, out, stream)
+    if r is not None:
+        return r
+    stride = _check_rows(y, "y")
+    code = _dtype_code(y.dtype)
+    rows, top = _check_slots(places, "places")
+    if y.shape[0] != rows * top:
+        raise ValueError("y must have as many rows as there are places")
+    _check_sizes(y.shape[1])
+    if weights is not None:
+        _check_floats(weights, "weights", (rows, top))
+    out, out_stride = _new_or_checked(out, "out", (rows, y.shape[1]), y.dtype, y, stream)
+    _done(lib.spinner_combine(y.data_ptr(), code, rows, y.shape[1], stride, places.data_ptr(), None if weights is None else weights.data_ptr(), top,
+                              out.data_ptr(), out_stride, _stream_handle(stream)))
+    return out
+
+
+def spinner_combine_grad(dout, y, places, weights, dy=None, dweights=None, stream=None):
+    """Gradients of spinner_combine: dy[places[r][j]] = weights[r][j] dout[r] of the type of y, and dweights[r][j] = dout[r] . y[places[r][j]] in fp32."""
+    r = _native_experts.combine_grad(dout, y, places, weights, dy, dweights, stream)
+    if r is not None:
+        return r
+    dout_stride, y_stride = _check_rows(dout, "dout"), _check_rows(y, "y", dout.dtype)
+    code = _dtype_code(y.dtype)
+    rows, top = _check_slots(places, "places")
+    if dout.shape[0] != rows or tuple(y.shape) != (rows * top, dout.shape[1]):
+        raise ValueError("dout and y must be rows of the same width, as many as places has rows and numbers")
+    _check_sizes(y.shape[1])
+    _check_floats(weights, "weights", (rows, top))
+    dy, dy_stride = _new_or_checked(dy, "dy", tuple(y.shape), y.dtype, y, stream)
+    if dweights is None:
+        dweights = _new((rows, top), torch.float32, y.device, stream)
+    _check_floats(dweights, "dweights", (rows, top))
+    _done(lib.spinner_combine_grad(dout.data_ptr(), y.data_ptr(), code, rows, y.shape[1], dout_stride, y_stride, places.data_ptr(), weights.data_ptr(), top,
+                                   dy.data_ptr(), dy_stride, dweights.data_ptr(), _stream_handle(stream)))
+    return dy, dweights

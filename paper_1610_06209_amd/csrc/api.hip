@@ -10,7 +10,9 @@
 
 #include "launch.hpp"
 #include "layer_params.hpp"
+#include "int_rows.hpp"
 #include "mx4.hpp"
+#include "route.hpp"
 
 namespace spinner {
 // ------------------------------------------------------------------ plain copy (measurement aid)
@@ -1089,6 +1091,290 @@ int spinner_grouped_matmul_dw(const void* dy, const void* x, int dtype, long row
     p.workspace = workspace;
     const auto launch = dtype == SPINNER_BF16 ? spinner::launch_product_bf16 : spinner::launch_product_f16;
     return launched(launch(spinner::kDw, dw_dtype, p, static_cast<hipStream_t>(stream)));
+}
+
+// ------------------------------------------------------------------ 8-bit whole numbers
+static bool int_depth(int k) { return k >= 1 && k <= spinner::kMostIntDepth; }
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// rows that go to `top` places each
+static int check_places(long rows, int top)
+{
+    if (top < 1 || top > spinner::kMostChosen) return SPINNER_ERR_BAD_SHAPE;
+    if (rows < 0 || rows > kMostRows / top) return SPINNER_ERR_BAD_BATCH;
+    return SPINNER_OK;
+}
+
+static int check_int_quantize(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block, const int* places, int top)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    const int rc = check_places(rows, top);
+    if (rc != SPINNER_OK) return rc;
+    if (!int_depth(k) || !stride_in(x_stride)) return SPINNER_ERR_BAD_SHAPE;
+    if (block && (block < 32 || block > spinner::kMaxRotation || (block & (block - 1)) || k % block)) return SPINNER_ERR_BAD_SHAPE;
+    if ((diag && !block) || (!places && top != 1)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows && !x) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(x) || !aligned16(diag) || !aligned4(places)) return SPINNER_ERR_ALIGNMENT;
+    return SPINNER_OK;
+}
+
+static spinner::IntQuantizeParams int_quantize_params(const void* x, long rows, int k, long x_stride, const float* diag, int block, const int* places, int top,
+                                                      void* codes, float* scales)
+{
+    spinner::IntQuantizeParams p = {};
+    p.x = x;
+    p.diag = diag;
+    p.codes = static_cast<int8_t*>(codes);
+    p.scales = scales;
+    p.places = places;
+    p.x_stride = x_stride;
+    p.rows = (int)rows;
+    p.k = k;
+    p.width = spinner::int_width(k);
+    p.top = top;
+    p.norm = block ? 1.0f / sqrtf((float)block) : 0.0f;
+    p.log = block ? __builtin_ctz(block) : 0;
+    return p;
+}
+
+int spinner_int_quantize(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block, const int* places, int top, void* codes,
+                         float* scales, void* stream)
+{
+    const int rc = check_int_quantize(x, dtype, rows, k, x_stride, diag, block, places, top);
+    if (rc != SPINNER_OK) return rc;
+    if (rows == 0) return SPINNER_OK;
+    if (!codes || !scales) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(codes) || !aligned4(scales)) return SPINNER_ERR_ALIGNMENT;
+    return launched(spinner::launch_int_quantize(int_quantize_params(x, rows, k, x_stride, diag, block, places, top, codes, scales), dtype,
+                                                 static_cast<hipStream_t>(stream)));
+}
+
+int spinner_int_dequantize(const void* codes, const float* scales, long rows, int k, void* out, int dtype, long out_stride, void* stream)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    if (rows < 0 || rows > kMostRows) return SPINNER_ERR_BAD_BATCH;
+    if (!int_depth(k) || !stride_out(out_stride, k, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!codes || !scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(codes) || !aligned4(scales) || !aligned16(out)) return SPINNER_ERR_ALIGNMENT;
+    return launched(spinner::launch_int_dequantize(static_cast<const int8_t*>(codes), scales, (int)rows, k, out, dtype, out_stride,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
+static spinner::ProductParams int_params(const void* a_codes, const float* a_scales, long rows, int k, const void* w_codes, const float* w_scales, int n,
+                                         int experts, const long long* ends, void* out, long out_stride)
+{
+    spinner::ProductParams p = {};
+    p.a = static_cast<const char*>(a_codes);
+    p.b = static_cast<const char*>(w_codes);
+    p.a_scales = reinterpret_cast<const uint8_t*>(a_scales);
+    p.b_scales = reinterpret_cast<const uint8_t*>(w_scales);
+    p.out = static_cast<char*>(out);
+    p.ends = ends;
+    p.depth = spinner::int_width(k);
+    p.a_stride = p.b_stride = p.depth;
+    p.b_group = (long long)n * p.depth;
+    p.out_stride = out_stride;
+    p.rows = (int)rows;
+    p.experts = experts;
+    p.width = n;
+    spinner::plan_product_int(&p);
+    return p;
+}
+
+int spinner_int_matmul(const void* a_codes, const float* a_scales, long rows, int k, const void* w_codes, const float* w_scales, int n, int experts,
+                       const long long* ends, void* out, int dtype, long out_stride, void* stream)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    const int rc = check_groups(rows, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    if (!int_depth(k) || !side(n) || !stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(a_codes) || !aligned16(w_codes) || !aligned16(out) || !aligned4(a_scales) || !aligned4(w_scales)) return SPINNER_ERR_ALIGNMENT;
+    const spinner::ProductParams p = int_params(a_codes, a_scales, rows, k, w_codes, w_scales, n, experts, ends, out, out_stride);
+    return launched(spinner::launch_product_int(dtype, p, static_cast<hipStream_t>(stream)));
+}
+
+size_t spinner_int_linear_workspace_bytes(long rows, int k)
+{
+    if (rows < 0 || rows > kMostRows || !int_depth(k)) return 0;
+    return (size_t)rows * (spinner::int_width(k) + sizeof(float));
+}
+
+int spinner_int_linear(const void* x, int dtype, long rows, int k, long x_stride, const float* diag, int block, const int* places, int top,
+                       const void* w_codes, const float* w_scales, int n, int experts, const long long* ends, void* out, long out_stride, void* workspace,
+                       void* stream)
+{
+    int rc = check_int_quantize(x, dtype, rows, k, x_stride, diag, block, places, top);
+    const long slots = rc == SPINNER_OK ? rows * top : 0;
+    if (rc == SPINNER_OK) rc = check_groups(slots, experts, ends);
+    if (rc != SPINNER_OK) return rc;
+    if (!side(n) || !stride_out(out_stride, n, slots)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!w_codes || !w_scales || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(w_codes) || !aligned4(w_scales) || !aligned16(out) || !aligned16(workspace)) return SPINNER_ERR_ALIGNMENT;
+    char* codes = static_cast<char*>(workspace);
+    float* scales = codes ? reinterpret_cast<float*>(codes + (size_t)slots * spinner::int_width(k)) : nullptr;
+    const spinner::ProductParams p = int_params(codes, scales, slots, k, w_codes, w_scales, n, experts, ends, out, out_stride);
+    const spinner::IntQuantizeParams q = int_quantize_params(x, rows, k, x_stride, diag, block, places, top, codes, scales);
+    if (!places && spinner::int_quantises_within(p)) {
+        const spinner::RawRows raw = {x, diag, x_stride, q.norm, q.log, k};
+        return launched(spinner::launch_product_int_raw(dtype, p, raw, static_cast<hipStream_t>(stream)));
+    }
+    if (!workspace) return SPINNER_ERR_WORKSPACE;
+    rc = launched(spinner::launch_int_quantize(q, dtype, static_cast<hipStream_t>(stream)));
+    if (rc != SPINNER_OK) return rc;
+    return launched(spinner::launch_product_int(dtype, p, static_cast<hipStream_t>(stream)));
+}
+
+// ------------------------------------------------------------------ routing
+static_assert(SPINNER_SCORE_SOFTMAX == spinner::kSoftmax && SPINNER_SCORE_SIGMOID == spinner::kSigmoid, "the scores");
+
+static int check_route(int dtype, long rows, int experts, long stride, int score, int top)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    if (experts < 1 || experts > spinner::kMostRouted || top > experts || !stride_in(stride)) return SPINNER_ERR_BAD_SHAPE;
+    if (score != SPINNER_SCORE_SOFTMAX && score != SPINNER_SCORE_SIGMOID) return SPINNER_ERR_BAD_EPILOGUE;
+    return check_places(rows, top);
+}
+
+int spinner_route(const void* logits, int dtype, long rows, int experts, long stride, const float* bias, const void* mask, int score, int groups,
+                  int top_groups, int group_top, int top, int renormalise, float scale, float* weights, int* chosen, void* stream)
+{
+    const int rc = check_route(dtype, rows, experts, stride, score, top);
+    if (rc != SPINNER_OK) return rc;
+    if (groups < 1 || groups > spinner::kMostRouteGroups || experts % groups || top_groups < 1 || top_groups > groups) return SPINNER_ERR_BAD_SHAPE;
+    if (group_top < 1 || group_top > 2 || top > top_groups * (experts / groups)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!logits || !weights || !chosen) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(logits) || !aligned4(bias) || !aligned4(weights) || !aligned4(chosen)) return SPINNER_ERR_ALIGNMENT;
+    spinner::RouteParams p = {};
+    p.logits = logits;
+    p.bias = bias;
+    p.mask = static_cast<const uint8_t*>(mask);
+    p.weights = weights;
+    p.experts = chosen;
+    p.stride = stride;
+    p.rows = (int)rows;
+    p.count = experts;
+    p.top = top;
+    p.groups = groups;
+    p.top_groups = top_groups;
+    p.group_top = groups > 1 ? group_top : 1;
+    p.score = score;
+    p.renormalise = renormalise;
+    p.scale = scale;
+    return launched(spinner::launch_route(p, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int spinner_route_grad(const float* dweights, const void* logits, int dtype, long rows, int experts, long stride, const int* chosen, int score, int top,
+                       int renormalise, float scale, void* dlogits, long dlogits_stride, void* stream)
+{
+    const int rc = check_route(dtype, rows, experts, stride, score, top);
+    if (rc != SPINNER_OK) return rc;
+    if (!stride_out(dlogits_stride, experts, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!dweights || !logits || !chosen || !dlogits) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(logits) || !aligned16(dlogits) || !aligned4(dweights) || !aligned4(chosen)) return SPINNER_ERR_ALIGNMENT;
+    spinner::RouteParams p = {};
+    p.logits = logits;
+    p.experts = const_cast<int*>(chosen);
+    p.dweights = dweights;
+    p.dlogits = dlogits;
+    p.stride = stride;
+    p.dstride = dlogits_stride;
+    p.rows = (int)rows;
+    p.count = experts;
+    p.top = top;
+    p.groups = p.top_groups = p.group_top = 1;
+    p.score = score;
+    p.renormalise = renormalise;
+    p.scale = scale;
+    return launched(spinner::launch_route_grad(p, dtype, static_cast<hipStream_t>(stream)));
+}
+
+static bool order_sizes(long count, int experts) { return count >= 0 && count <= kMostRows && experts >= 1 && experts <= spinner::kMostRouted; }
+static spinner::OrderParams order_params(long count, int experts)
+{
+    spinner::OrderParams p = {};
+    p.entries = (int)count;
+    p.count = experts;
+    spinner::plan_order(&p);
+    return p;
+}
+
+size_t spinner_route_order_workspace_bytes(long count, int experts)
+{
+    if (!order_sizes(count, experts)) return 0;
+    const spinner::OrderParams p = order_params(count, experts);
+    return p.blocks > 1 ? (size_t)p.blocks * (experts + 1) * sizeof(int) : 0;
+}
+
+int spinner_route_order(const int* chosen, long count, int experts, int* places, long long* ends, void* workspace, void* stream)
+{
+    if (!order_sizes(count, experts)) return count < 0 || count > kMostRows ? SPINNER_ERR_BAD_BATCH : SPINNER_ERR_BAD_SHAPE;
+    if (!ends || (count && (!chosen || !places))) return SPINNER_ERR_NULL_PTR;
+    spinner::OrderParams p = order_params(count, experts);
+    if (p.blocks > 1 && !workspace) return SPINNER_ERR_WORKSPACE;
+    if (!aligned4(chosen) || !aligned4(places) || (reinterpret_cast<uintptr_t>(ends) & 7u) || !aligned4(workspace)) return SPINNER_ERR_ALIGNMENT;
+    p.experts = chosen;
+    p.places = places;
+    p.ends = ends;
+    p.counts = p.blocks > 1 ? static_cast<int*>(workspace) : nullptr;
+    return launched(spinner::launch_order(p, static_cast<hipStream_t>(stream)));
+}
+
+static int check_exchange(int dtype, long rows, int n, long stride, int top)
+{
+    if (!plain_type(dtype)) return SPINNER_ERR_BAD_TYPE;
+    if (!side(n) || !stride_in(stride)) return SPINNER_ERR_BAD_SHAPE;
+    return check_places(rows, top);
+}
+static spinner::ExchangeParams exchange_params(const void* x, const void* y, void* out, const int* places, const float* weights, float* dweights,
+                                               int dtype, long x_stride, long y_stride, long out_stride, long rows, int top, int n)
+{
+    const long long size = dtype == SPINNER_F32 ? 4 : 2;
+    return {static_cast<const char*>(x), static_cast<const char*>(y), static_cast<char*>(out), places, weights, dweights,
+            x_stride * size, y_stride * size, out_stride * size, (int)rows, top, n};
+}
+
+int spinner_dispatch(const void* x, int dtype, long rows, int n, long x_stride, const int* places, int top, void* out, long out_stride, void* stream)
+{
+    const int rc = check_exchange(dtype, rows, n, x_stride, top);
+    if (rc != SPINNER_OK) return rc;
+    if (!stride_out(out_stride, n, rows * top)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!x || !places || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(x) || !aligned16(out) || !aligned4(places)) return SPINNER_ERR_ALIGNMENT;
+    const spinner::ExchangeParams p = exchange_params(x, nullptr, out, places, nullptr, nullptr, dtype, x_stride, 0, out_stride, rows, top, n);
+    return launched(spinner::launch_dispatch(p, dtype == SPINNER_F32 ? 4 : 2, static_cast<hipStream_t>(stream)));
+}
+
+int spinner_combine(const void* y, int dtype, long rows, int n, long y_stride, const int* places, const float* weights, int top, void* out,
+                    long out_stride, void* stream)
+{
+    const int rc = check_exchange(dtype, rows, n, y_stride, top);
+    if (rc != SPINNER_OK) return rc;
+    if (!stride_out(out_stride, n, rows)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!y || !places || !out) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(y) || !aligned16(out) || !aligned4(places) || !aligned4(weights)) return SPINNER_ERR_ALIGNMENT;
+    const spinner::ExchangeParams p = exchange_params(y, nullptr, out, places, weights, nullptr, dtype, y_stride, 0, out_stride, rows, top, n);
+    return launched(spinner::launch_combine(p, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int spinner_combine_grad(const void* dout, const void* y, int dtype, long rows, int n, long dout_stride, long y_stride, const int* places,
+                         const float* weights, int top, void* dy, long dy_stride, float* dweights, void* stream)
+{
+    const int rc = check_exchange(dtype, rows, n, dout_stride, top);
+    if (rc != SPINNER_OK) return rc;
+    if (!stride_in(y_stride) || !stride_out(dy_stride, n, rows * top)) return SPINNER_ERR_BAD_SHAPE;
+    if (rows == 0) return SPINNER_OK;
+    if (!dout || !y || !places || !weights || !dy || !dweights) return SPINNER_ERR_NULL_PTR;
+    if (!aligned16(dout) || !aligned16(y) || !aligned16(dy) || !aligned4(places) || !aligned4(weights) || !aligned4(dweights)) return SPINNER_ERR_ALIGNMENT;
+    const spinner::ExchangeParams p = exchange_params(dout, y, dy, places, weights, dweights, dtype, dout_stride, y_stride, dy_stride, rows, top, n);
+    return launched(spinner::launch_combine_grad(p, dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

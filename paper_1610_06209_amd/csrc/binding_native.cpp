@@ -733,6 +733,278 @@ ENTRY(grouped_matmul_dw, 7)
     return THPVariable_Wrap(std::move(dw));
 ENTRY_END
 
+// ------------------------------------------------------------------ 8-bit whole numbers
+int64_t int_width(int64_t k) { return (k + 15) / 16 * 16; }
+PyObject* two(Tensor&& a, Tensor&& b)
+{
+    PyObject *x = THPVariable_Wrap(std::move(a)), *y = x ? THPVariable_Wrap(std::move(b)) : nullptr;
+    if (!y) { Py_XDECREF(x); return nullptr; }
+    PyObject* both = PyTuple_Pack(2, x, y);
+    Py_DECREF(x);
+    Py_DECREF(y);
+    return both;
+}
+const Tensor* shaped(PyObject* o, at::ScalarType type, at::IntArrayRef sizes)
+{
+    const Tensor* t = here(o, type);
+    return t && t->sizes() == sizes ? t : nullptr;
+}
+// memory that the caller may bring, of this shape
+bool given_as(PyObject* o, const Tensor** t, at::ScalarType type, at::IntArrayRef sizes)
+{
+    *t = nullptr;
+    return o == Py_None || (*t = shaped(o, type, sizes));
+}
+bool places_of(PyObject* o, long rows, const int** p, int* top)
+{
+    *p = nullptr;
+    *top = 1;
+    if (o == Py_None) return true;
+    const Tensor* t = here(o, at::kInt);
+    if (!t || t->dim() != 2 || t->size(0) != rows || t->size(1) < 1 || t->size(1) > 32 || rows > INT_MAX) return false;
+    *p = ptr<const int>(t);
+    *top = (int)t->size(1);
+    return true;
+}
+bool int_weights(PyObject* codes, PyObject* scales, int64_t width, int* experts, int* n, const Tensor** wc, const Tensor** ws)
+{
+    int64_t w;
+    *wc = here(codes, at::kChar);
+    *ws = here(scales, at::kFloat);
+    return weights(*wc, experts, n, &w) && w == width && *ws && (*ws)->sizes() == (*wc)->sizes().slice(0, (*wc)->dim() - 1);
+}
+
+// x, diag, block, places, codes, scales, stream
+ENTRY(int_quantize, 7)
+    long count;
+    int k, code, block, top;
+    const int* places;
+    const Tensor *x = number_rows(a[0], &count, &k, &code), *d, *gc, *gs;
+    if (!x || a[6] != Py_None || !rotation(a[1], a[2], k, &d, &block) || !places_of(a[3], count, &places, &top)) LONG_WAY;
+    const int64_t slots = count * top, width = int_width(k);
+    if (!given_as(a[4], &gc, at::kChar, {slots, width}) || !given_as(a[5], &gs, at::kFloat, {slots})) LONG_WAY;
+    Tensor codes, scales;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        codes = result(gc, {slots, width}, at::kChar, *x);
+        scales = result(gs, {slots}, at::kFloat, *x);
+        rc = spinner_int_quantize(ptr<void>(x), code, count, k, k, ptr(d), block, places, top, ptr<void>(codes), ptr(scales), current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return two(std::move(codes), std::move(scales));
+ENTRY_END
+
+// codes, scales, dtype, k, out, stream
+ENTRY(int_dequantize, 6)
+    const Tensor *codes = here(a[0], at::kChar), *given;
+    at::ScalarType type;
+    int code, k;
+    if (!codes || codes->dim() != 2 || codes->size(1) > INT_MAX || a[5] != Py_None || !dtype_of(a[2], &type, &code)) LONG_WAY;
+    const long count = (long)codes->size(0);
+    if (a[3] == Py_None) k = (int)codes->size(1);
+    else if (!whole(a[3], &k)) LONG_WAY;
+    const Tensor* scales = shaped(a[1], at::kFloat, {count});
+    if (!scales || int_width(k) != codes->size(1) || !result_rows(a[4], &given, type, count, k)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, k}, type, *codes);
+        rc = spinner_int_dequantize(ptr<void>(codes), ptr(scales), count, k, ptr<void>(out), code, k, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// a_codes, a_scales, w_codes, w_scales, ends, dtype, out, stream
+ENTRY(int_matmul, 8)
+    const Tensor *codes = here(a[0], at::kChar), *wc, *ws, *given;
+    at::ScalarType type;
+    int code, experts, n;
+    const long long* ends;
+    if (!codes || codes->dim() != 2 || codes->size(1) % 16 || codes->size(1) > INT_MAX || a[7] != Py_None || !dtype_of(a[5], &type, &code)) LONG_WAY;
+    const long count = (long)codes->size(0);
+    const int k = (int)codes->size(1);
+    const Tensor* scales = shaped(a[1], at::kFloat, {count});
+    if (!scales || !int_weights(a[2], a[3], k, &experts, &n, &wc, &ws) || !expert_ends(a[4], experts, &ends) || !result_rows(a[6], &given, type, count, n)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, n}, type, *codes);
+        rc = spinner_int_matmul(ptr<void>(codes), ptr(scales), count, k, ptr<void>(wc), ptr(ws), n, experts, ends, ptr<void>(out), code, n, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// x, w_codes, w_scales, diag, block, ends, places, out, workspace, stream
+ENTRY(int_linear, 10)
+    long count;
+    int k, code, block, experts, n, top;
+    const long long* ends;
+    const int* places;
+    const Tensor *x = number_rows(a[0], &count, &k, &code), *wc, *ws, *d, *given;
+    if (!x || a[9] != Py_None || !rotation(a[3], a[4], k, &d, &block) || !int_weights(a[1], a[2], int_width(k), &experts, &n, &wc, &ws)) LONG_WAY;
+    if (!expert_ends(a[5], experts, &ends) || !places_of(a[6], count, &places, &top)) LONG_WAY;
+    const long slots = count * top;
+    if (!result_rows(a[7], &given, x->scalar_type(), slots, n)) LONG_WAY;
+    const size_t need = spinner_int_linear_workspace_bytes(slots, k);
+    Buffer w;
+    if ((a[8] != Py_None && !here(a[8])) || !w.usable_bytes(a[8], need)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {slots, n}, x->scalar_type(), *x);
+        const auto call = [&](void* scratch) {
+            return spinner_int_linear(ptr<void>(x), code, count, k, k, ptr(d), block, places, top, ptr<void>(wc), ptr(ws), n, experts, ends, ptr<void>(out), n,
+                                      scratch, current_stream());
+        };
+        // (a few rows need none)
+        rc = call(ptr<void>(w.given));
+        if (rc == SPINNER_ERR_WORKSPACE) rc = call(ptr<void>(w.scratch(need, *x)));
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// ------------------------------------------------------------------ routing
+bool score_of(PyObject* o, int* v)
+{
+    static const char* const names[] = {"softmax", "sigmoid"};
+    static_assert(SPINNER_SCORE_SOFTMAX == 0 && SPINNER_SCORE_SIGMOID == 1, "the order of the names");
+    return choice(o, names, 2, v);
+}
+
+// logits, top, bias, mask, score, groups, top_groups, group_top, renormalise, scale, weights, experts, stream
+ENTRY(route, 13)
+    long count;
+    int width, code, top, score, groups, top_groups, group_top;
+    float scale;
+    const Tensor *x = number_rows(a[0], &count, &width, &code), *bias = nullptr, *mask = nullptr, *gw, *ge;
+    if (!x || a[12] != Py_None || !whole(a[1], &top) || top < 1 || !score_of(a[4], &score) || !whole(a[5], &groups) || !whole(a[6], &top_groups)) LONG_WAY;
+    if (!whole(a[7], &group_top) || !PyBool_Check(a[8]) || !number(a[9], &scale)) LONG_WAY;
+    if (a[2] != Py_None && !(bias = shaped(a[2], at::kFloat, {width}))) LONG_WAY;
+    if (a[3] != Py_None && !(mask = shaped(a[3], at::kBool, {count}))) LONG_WAY;
+    if (!given_as(a[10], &gw, at::kFloat, {count, top}) || !given_as(a[11], &ge, at::kInt, {count, top})) LONG_WAY;
+    Tensor w, e;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        w = result(gw, {count, top}, at::kFloat, *x);
+        e = result(ge, {count, top}, at::kInt, *x);
+        rc = spinner_route(ptr<void>(x), code, count, width, width, ptr(bias), ptr<void>(mask), score, groups, top_groups, group_top, top, a[8] == Py_True, scale,
+                           ptr(w), ptr<int>(e), current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return two(std::move(w), std::move(e));
+ENTRY_END
+
+// dweights, logits, experts, score, renormalise, scale, dlogits, stream
+ENTRY(route_grad, 8)
+    long count;
+    int width, code, score;
+    float scale;
+    const Tensor *x = number_rows(a[1], &count, &width, &code), *e = here(a[2], at::kInt), *given;
+    if (!x || !e || e->dim() != 2 || e->size(0) != count || e->size(1) > INT_MAX || a[7] != Py_None || !score_of(a[3], &score)) LONG_WAY;
+    const Tensor* dw = shaped(a[0], at::kFloat, e->sizes());
+    if (!dw || !PyBool_Check(a[4]) || !number(a[5], &scale) || !result_rows(a[6], &given, x->scalar_type(), count, width)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, width}, x->scalar_type(), *x);
+        rc = spinner_route_grad(ptr(dw), ptr<void>(x), code, count, width, width, ptr<int>(e), score, (int)e->size(1), a[4] == Py_True, scale, ptr<void>(out), width,
+                                current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// experts, count, places, ends, workspace, stream
+ENTRY(route_order, 6)
+    const Tensor *e = here(a[0], at::kInt), *gp, *ge;
+    int experts;
+    if (!e || e->dim() != 2 || a[5] != Py_None || !whole(a[1], &experts) || experts < 1) LONG_WAY;
+    if (!given_as(a[2], &gp, at::kInt, e->sizes()) || !given_as(a[3], &ge, at::kLong, {experts})) LONG_WAY;
+    const size_t need = spinner_route_order_workspace_bytes((long)e->numel(), experts);
+    Buffer w;
+    if ((a[4] != Py_None && !here(a[4])) || !w.usable_bytes(a[4], need)) LONG_WAY;
+    Tensor places, ends;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        places = result(gp, e->sizes(), at::kInt, *e);
+        ends = result(ge, {experts}, at::kLong, *e);
+        const Tensor scratch = w.scratch(need, *e);
+        rc = spinner_route_order(ptr<int>(e), (long)e->numel(), experts, ptr<int>(places), ptr<long long>(ends), ptr<void>(scratch), current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return two(std::move(places), std::move(ends));
+ENTRY_END
+
+// x, places, out, stream
+ENTRY(dispatch, 4)
+    long count;
+    int n, code, top;
+    const int* places;
+    const Tensor *x = number_rows(a[0], &count, &n, &code), *given;
+    if (!x || a[3] != Py_None || a[1] == Py_None || !places_of(a[1], count, &places, &top) || !result_rows(a[2], &given, x->scalar_type(), count * top, n)) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count * top, n}, x->scalar_type(), *x);
+        rc = spinner_dispatch(ptr<void>(x), code, count, n, n, places, top, ptr<void>(out), n, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// y, places, weights, out, stream
+ENTRY(combine, 5)
+    long slots;
+    int n, code, top;
+    const int* places;
+    const Tensor *y = number_rows(a[0], &slots, &n, &code), *p = here(a[1], at::kInt), *w = nullptr, *given;
+    if (!y || !p || p->dim() != 2 || p->numel() != slots || a[4] != Py_None) LONG_WAY;
+    const long count = (long)p->size(0);
+    if (!places_of(a[1], count, &places, &top) || !result_rows(a[3], &given, y->scalar_type(), count, n)) LONG_WAY;
+    if (a[2] != Py_None && !(w = shaped(a[2], at::kFloat, {count, top}))) LONG_WAY;
+    Tensor out;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        out = result(given, {count, n}, y->scalar_type(), *y);
+        rc = spinner_combine(ptr<void>(y), code, count, n, n, places, ptr(w), top, ptr<void>(out), n, current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return THPVariable_Wrap(std::move(out));
+ENTRY_END
+
+// dout, y, places, weights, dy, dweights, stream
+ENTRY(combine_grad, 7)
+    long count, slots;
+    int n, code, y_n, y_code, top;
+    const int* places;
+    const Tensor *d = number_rows(a[0], &count, &n, &code), *y = number_rows(a[1], &slots, &y_n, &y_code), *gy, *gw;
+    if (!d || !y || y_n != n || y_code != code || a[6] != Py_None || a[2] == Py_None || !places_of(a[2], count, &places, &top) || slots != count * top) LONG_WAY;
+    const Tensor* w = shaped(a[3], at::kFloat, {count, top});
+    if (!w || !given_as(a[4], &gy, y->scalar_type(), {slots, n}) || !given_as(a[5], &gw, at::kFloat, {count, top})) LONG_WAY;
+    Tensor dy, dw;
+    int rc;
+    {
+        pybind11::gil_scoped_release free;
+        dy = result(gy, {slots, n}, y->scalar_type(), *y);
+        dw = result(gw, {count, top}, at::kFloat, *y);
+        rc = spinner_combine_grad(ptr<void>(d), ptr<void>(y), code, count, n, n, n, places, ptr(w), top, ptr<void>(dy), n, ptr(dw), current_stream());
+    }
+    if (rc != SPINNER_OK) return refused(rc);
+    return two(std::move(dy), std::move(dw));
+ENTRY_END
+
 #define METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(apply_signs), METHOD(apply), METHOD(apply_blocks), METHOD(hash), METHOD(hash_signs), METHOD(sign_codes),
                          METHOD(sign_codes_signs), METHOD(angular_gram), METHOD(layer_forward), METHOD(layer_backward), METHOD(sketch),
@@ -742,14 +1014,23 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods
 PyMethodDef product_methods[] = {METHOD(mx_quantize), METHOD(mx_dequantize), METHOD(mx_matmul), METHOD(mx_linear), METHOD(grouped_matmul),
                                  METHOD(grouped_matmul_dx), METHOD(grouped_matmul_dw), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef product_module_def = {PyModuleDef_HEAD_INIT, "_native._products", nullptr, -1, product_methods, nullptr, nullptr, nullptr, nullptr};
+// and those of routing and of 8-bit layers
+PyMethodDef expert_methods[] = {METHOD(int_quantize), METHOD(int_dequantize), METHOD(int_matmul), METHOD(int_linear), METHOD(route), METHOD(route_grad),
+                                METHOD(route_order), METHOD(dispatch), METHOD(combine), METHOD(combine_grad), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef expert_module_def = {PyModuleDef_HEAD_INIT, "_native._experts", nullptr, -1, expert_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__native()
 {
-    PyObject *module = PyModule_Create(&module_def), *products = module ? PyModule_Create(&product_module_def) : nullptr;
-    if (!products || PyModule_AddObject(module, "_products", products) != 0) {
-        Py_XDECREF(products);
+    PyObject* module = PyModule_Create(&module_def);
+    const auto add = [&](const char* name, PyModuleDef* def) {
+        PyObject* inner = module ? PyModule_Create(def) : nullptr;
+        if (inner && PyModule_AddObject(module, name, inner) == 0) return true;
+        Py_XDECREF(inner);
+        return false;
+    };
+    if (!add("_products", &product_module_def) || !add("_experts", &expert_module_def)) {
         Py_XDECREF(module);
         return nullptr;
     }

@@ -1,0 +1,278 @@
+// Rows to their places in the order of the experts, their weighted sums back, and the gradients of both.
+#include "mx4.hpp"
+#include "number_io.hpp"
+#include "route.hpp"
+#include "spinner_kernels.hpp"
+
+namespace spinner {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr long long kExchangeBlocks = 1 << 22;       // most workgroups: a grid holds fewer than 2^32 threads, and goes down the rows
+
+__device__ __forceinline__ Quad load_piece(const char* p)
+{
+    return *reinterpret_cast<const LooseQuad<2>::type*>(p);
+}
+__device__ __forceinline__ void write_piece(char* p, Quad v) { *reinterpret_cast<LooseQuad<2>::type*>(p) = v; }
+
+// A row of `bytes` in pieces of 16: where piece i starts (the last one ends with the row and may cover bytes of the one in front once more).
+__device__ __forceinline__ long long piece_start(long long i, long long bytes) { return i * 16 + 16 <= bytes ? i * 16 : bytes - 16; }
+
+// Geometry: LANES threads a row (256: one of blockIdx.y runs of 256 pieces), rows in turn over the grid.
+template <int LANES>
+struct RowsOfGrid {
+    long long row, step;
+    int lane;
+    long long first_piece, pieces_step;
+    __device__ __forceinline__ RowsOfGrid()
+    {
+        constexpr int ROWS = kThreads / LANES;
+        row = (long long)blockIdx.x * ROWS + (LANES == 256 ? 0 : threadIdx.x / LANES);
+        step = (long long)gridDim.x * ROWS;
+        lane = threadIdx.x & (LANES - 1);
+        first_piece = (long long)blockIdx.y * LANES + lane;
+        pieces_step = (long long)gridDim.y * LANES;
+    }
+};
+
+template <int SIZE, int LANES>
+__global__ void __launch_bounds__(kThreads) dispatch_kernel(ExchangeParams p)
+{
+    RowsOfGrid<LANES> at;
+    const long long bytes = (long long)p.n * SIZE, slots = (long long)p.rows * p.top;
+    for (; at.row < p.rows; at.row += at.step) {
+        const char* x = p.x + at.row * p.x_stride;
+        const int* places = p.places + at.row * p.top;
+        if (bytes >= 16) {
+            for (long long i = at.first_piece; i * 16 < bytes; i += at.pieces_step) {
+                const long long from = piece_start(i, bytes);
+                const Quad v = load_piece(x + from);
+                for (int j = 0; j < p.top; ++j) {
+                    const int place = places[j];
+                    if (place >= 0 && place < slots) write_piece(p.out + place * p.out_stride + from, v);
+                }
+            }
+        } else if (at.first_piece < p.n) {
+            using Number = std::conditional_t<SIZE == 4, unsigned, unsigned short>;
+            const Number v = reinterpret_cast<const Number*>(x)[at.first_piece];
+            for (int j = 0; j < p.top; ++j) {
+                const int place = places[j];
+                if (place >= 0 && place < slots) reinterpret_cast<Number*>(p.out + place * p.out_stride)[at.first_piece] = v;
+            }
+        }
+    }
+}
+
+// 16 bytes of numbers in fp32
+template <typename T, int N = 16 / (int)sizeof(T)>
+__device__ __forceinline__ void widen(Quad q, float (&v)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(q[k]);
+        else v[k] = (float)__builtin_bit_cast(typename Pair16<T>::Pair, (unsigned)q[k >> 1])[k & 1];
+    }
+}
+
+// out[r] = sum_j w[r][j] y[places[r][j]], fp32, j in order.  What has the weight 0 adds nothing, whatever its row holds: a choice of no expert has it,
+// and its row may never have been written.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kThreads) combine_kernel(ExchangeParams p)
+{
+    constexpr int N = 16 / (int)sizeof(T), GROUP = 4;
+    RowsOfGrid<LANES> at;
+    const long long bytes = (long long)p.n * sizeof(T), slots = (long long)p.rows * p.top;
+    for (; at.row < p.rows; at.row += at.step) {
+        const int* places = p.places + at.row * p.top;
+        const float* weights = p.weights ? p.weights + at.row * p.top : nullptr;
+        char* out = p.out + at.row * p.out_stride;
+        if (bytes >= 16) {
+            for (long long i = at.first_piece; i * 16 < bytes; i += at.pieces_step) {
+                const long long from = piece_start(i, bytes);
+                float sum[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = 0.0f;
+                for (int j0 = 0; j0 < p.top; j0 += GROUP) {
+                    Quad q[GROUP];
+                    float w[GROUP];
+                    bool there[GROUP];
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g) {
+                        const int j = j0 + g < p.top ? j0 + g : p.top - 1, place = places[j];
+                        w[g] = weights ? weights[j] : 1.0f;
+                        there[g] = j0 + g < p.top && place >= 0 && place < slots && w[g] != 0.0f;
+                        q[g] = load_piece(p.x + (there[g] ? place : 0) * p.x_stride + from);
+                    }
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g) {
+                        float v[N];
+                        widen<T>(q[g], v);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) sum[k] = there[g] ? __builtin_fmaf(w[g], v[k], sum[k]) : sum[k];
+                    }
+                }
+                store_quad(reinterpret_cast<T*>(out + from), sum);
+            }
+        } else if (at.first_piece < p.n) {
+            float sum = 0.0f;
+            for (int j = 0; j < p.top; ++j) {
+                const int place = places[j];
+                const float w = weights ? weights[j] : 1.0f;
+                if (place >= 0 && place < slots && w != 0.0f) sum = __builtin_fmaf(w, (float)reinterpret_cast<const T*>(p.x + place * p.x_stride)[at.first_piece], sum);
+            }
+            reinterpret_cast<T*>(out)[at.first_piece] = (T)sum;
+        }
+    }
+}
+
+// dy[places[r][j]] = w[r][j] dout[r], dw[r][j] = sum_i dout[r][i] y[places[r][j]][i]: a workgroup (or LANES of its lanes) a row, a few j at a time
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kThreads) combine_grad_kernel(ExchangeParams p)
+{
+    constexpr int N = 16 / (int)sizeof(T), GROUP = 4, ROWS = kThreads / LANES;
+    __shared__ float part[kThreads / 64][GROUP];
+    const int lane = threadIdx.x & (LANES - 1), wave = threadIdx.x >> 6;
+    const long long bytes = (long long)p.n * sizeof(T), slots = (long long)p.rows * p.top;
+    for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
+        const long long own = r0 + (LANES == 256 ? 0 : threadIdx.x / LANES), row = own < p.rows ? own : p.rows - 1;
+        const char* dout = p.x + row * p.x_stride;
+        for (int j0 = 0; j0 < p.top; j0 += GROUP) {
+            long long place[GROUP];
+            float w[GROUP], dot[GROUP];
+            bool there[GROUP];
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) {
+                const int j = j0 + g < p.top ? j0 + g : p.top - 1;
+                place[g] = p.places[row * p.top + j];
+                there[g] = own < p.rows && j0 + g < p.top && place[g] >= 0 && place[g] < slots;
+                if (!there[g]) place[g] = 0;
+                w[g] = p.weights[row * p.top + j];
+                dot[g] = 0.0f;
+            }
+            if (bytes >= 16) {
+                for (long long i = lane; i * 16 < bytes; i += LANES) {
+                    const long long from = piece_start(i, bytes);
+                    const int again = (int)(i * 16 - from) / (int)sizeof(T);      // numbers that the piece in front has as well
+                    float d[N];
+                    const Quad qd = load_piece(dout + from);
+                    Quad q[GROUP];
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g) q[g] = load_piece(p.y + place[g] * p.y_stride + from);
+                    widen<T>(qd, d);
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g) {
+                        float v[N], t[N];
+                        widen<T>(q[g], v);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) {
+                            t[k] = w[g] * d[k];
+                            dot[g] = k >= again ? __builtin_fmaf(d[k], v[k], dot[g]) : dot[g];
+                        }
+                        if (there[g]) store_quad(reinterpret_cast<T*>(p.out + place[g] * p.out_stride + from), t);
+                    }
+                }
+            } else if (lane < p.n) {
+                const float d = (float)reinterpret_cast<const T*>(dout)[lane];
+#pragma unroll
+                for (int g = 0; g < GROUP; ++g)
+                    if (there[g]) {
+                        dot[g] = d * (float)reinterpret_cast<const T*>(p.y + place[g] * p.y_stride)[lane];
+                        reinterpret_cast<T*>(p.out + place[g] * p.out_stride)[lane] = (T)(w[g] * d);
+                    }
+            }
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) {
+                dot[g] += lane_xor<1>(dot[g]);
+                dot[g] += lane_xor<2>(dot[g]);
+                dot[g] += lane_xor<4>(dot[g]);
+                dot[g] += lane_xor<8>(dot[g]);
+                if constexpr (LANES > 16) {
+                    dot[g] += lane_xor<16>(dot[g]);
+                    dot[g] += lane_xor<32>(dot[g]);
+                }
+            }
+            if constexpr (LANES == 256) {
+                if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g) part[wave][g] = dot[g];
+                __syncthreads();
+                if (threadIdx.x < GROUP && j0 + (int)threadIdx.x < p.top) {
+                    const int g = threadIdx.x, j = j0 + g;
+                    const int at = p.places[row * p.top + j];
+                    const float all = (part[0][g] + part[1][g]) + (part[2][g] + part[3][g]);
+                    p.dweights[row * p.top + j] = at >= 0 && at < slots ? all : 0.0f;
+                }
+                __syncthreads();
+            } else if (lane == 0 && own < p.rows) {
+#pragma unroll
+                for (int g = 0; g < GROUP; ++g)
+                    if (j0 + g < p.top) p.dweights[row * p.top + j0 + g] = there[g] ? dot[g] : 0.0f;
+            }
+        }
+    }
+}
+
+// workgroups over rows and over the 256-piece runs of a long row
+dim3 grid_of(const ExchangeParams& p, int rows_each, long long runs)
+{
+    const long long want = (p.rows + rows_each - 1LL) / rows_each, most = kExchangeBlocks / runs > 0 ? kExchangeBlocks / runs : 1;
+    return dim3((unsigned)(want < most ? want : most), (unsigned)runs);
+}
+long long pieces_of(const ExchangeParams& p, int size)
+{
+    const long long bytes = (long long)p.n * size;
+    return bytes >= 16 ? (bytes + 15) / 16 : p.n;
+}
+
+template <int SIZE>
+hipError_t dispatch(const ExchangeParams& p, hipStream_t s)
+{
+    const long long pieces = pieces_of(p, SIZE);
+    if (pieces <= 16) hipLaunchKernelGGL((dispatch_kernel<SIZE, 16>), grid_of(p, 16, 1), dim3(kThreads), 0, s, p);
+    else if (pieces <= 128) hipLaunchKernelGGL((dispatch_kernel<SIZE, 64>), grid_of(p, 4, 1), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((dispatch_kernel<SIZE, 256>), grid_of(p, 1, pieces < 256 * 32768 ? (pieces + 255) / 256 : 32768), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t combine(const ExchangeParams& p, hipStream_t s)
+{
+    const long long pieces = pieces_of(p, sizeof(T));
+    if (pieces <= 16) hipLaunchKernelGGL((combine_kernel<T, 16>), grid_of(p, 16, 1), dim3(kThreads), 0, s, p);
+    else if (pieces <= 128) hipLaunchKernelGGL((combine_kernel<T, 64>), grid_of(p, 4, 1), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((combine_kernel<T, 256>), grid_of(p, 1, pieces < 256 * 32768 ? (pieces + 255) / 256 : 32768), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t combine_grad(const ExchangeParams& p, hipStream_t s)
+{
+    const long long pieces = pieces_of(p, sizeof(T));
+    if (pieces <= 16) hipLaunchKernelGGL((combine_grad_kernel<T, 16>), grid_of(p, 16, 1), dim3(kThreads), 0, s, p);
+    else if (pieces <= 128) hipLaunchKernelGGL((combine_grad_kernel<T, 64>), grid_of(p, 4, 1), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((combine_grad_kernel<T, 256>), grid_of(p, 1, 1), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_dispatch(const ExchangeParams& p, int size, hipStream_t s) { return size == 4 ? dispatch<4>(p, s) : dispatch<2>(p, s); }
+
+hipError_t launch_combine(const ExchangeParams& p, int dtype, hipStream_t s)
+{
+    switch (dtype) {
+    case kF32: return combine<float>(p, s);
+    case kBf16: return combine<__bf16>(p, s);
+    default: return combine<_Float16>(p, s);
+    }
+}
+
+hipError_t launch_combine_grad(const ExchangeParams& p, int dtype, hipStream_t s)
+{
+    switch (dtype) {
+    case kF32: return combine_grad<float>(p, s);
+    case kBf16: return combine_grad<__bf16>(p, s);
+    default: return combine_grad<_Float16>(p, s);
+    }
+}
+
+}  // namespace spinner

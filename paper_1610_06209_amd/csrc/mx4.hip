@@ -1,6 +1,7 @@
 // Rotation and quantisation to microscaled 4-bit floating point (e2m1 with a shared power of two for each 32 numbers), and back.
 #include <math.h>
 
+#include "int_rows.hpp"
 #include "mx4_lane.hpp"
 
 namespace spinner {
@@ -154,8 +155,9 @@ constexpr int kHeldDepth = 8192;
 constexpr size_t kMostPartial = 64u << 20;       // bytes of partial sums
 
 template <int N>
-static void shortest(const Form (&forms)[N], int direction, bool mx4, ProductParams* p)
+static void shortest(const Form (&forms)[N], int direction, int chunk_numbers, ProductParams* p)
 {
+    const bool mx4 = chunk_numbers == 256;
     double best = 1e30;
     for (const Form& f : forms) {
         if (mx4 && f.tile == kTile64 && p->depth > kHeldDepth) continue;
@@ -168,7 +170,7 @@ static void shortest(const Form (&forms)[N], int direction, bool mx4, ProductPar
         } else {
             // a group's last tile is half full on average
             tiles *= p->experts > 1 ? (double)p->rows / f.side + 0.5 * (p->experts < p->rows ? p->experts : p->rows) : (p->rows + f.side - 1) / f.side;
-            chunks = ceil(p->depth / (mx4 ? 256.0 : 64.0));
+            chunks = ceil((double)p->depth / chunk_numbers);
         }
         for (int splits = 1; splits <= (direction == kDw ? 16 : 1); splits *= 2) {
             const double work = tiles * splits, rounds = ceil(work / f.slots), share = ceil(chunks / splits);
@@ -204,9 +206,19 @@ void plan_product(int direction, bool mx4, ProductParams* p)
             return;
         }
     }
-    if (mx4) shortest(kForms4, direction, true, p);
-    else shortest(kForms16, direction, false, p);
+    if (mx4) shortest(kForms4, direction, 256, p);
+    else shortest(kForms16, direction, 64, p);
 }
+
+// (a chunk of 128 whole numbers takes the loads, reads and products of one of 64 numbers of 16 bits)
+void plan_product_int(ProductParams* p)
+{
+    p->splits = 1;
+    if ((p->rows + p->experts - 1) / p->experts <= 16) p->tile = kFewRows;
+    else shortest(kForms16, kForward, 128, p);
+}
+
+bool int_quantises_within(const ProductParams& p) { return quantises_within(p); }
 
 bool quantises_within(const ProductParams& p)
 {

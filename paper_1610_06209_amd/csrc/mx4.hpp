@@ -5,8 +5,8 @@
 
 namespace spinner {
 
-// element types, in the order of spinner_dtype_t; kMx4 is internal (4-bit operands)
-enum { kF32 = 0, kBf16 = 1, kF16 = 2, kMx4 = 3 };
+// element types, in the order of spinner_dtype_t; kMx4 and kInt8 are internal (operands of 4 bits and of 8-bit whole numbers)
+enum { kF32 = 0, kBf16 = 1, kF16 = 2, kMx4 = 3, kInt8 = 4 };
 
 constexpr int kMx4Block = 32;             // numbers that share a scale
 constexpr int kMaxRotation = 4096;        // longest run of coordinates that one rotation mixes
@@ -33,8 +33,8 @@ enum { kForward = 0,      // out[row][n] = sum_k a[row][k] b[e][n][k]
 struct ProductParams {
     const char* a;                        // operand of the result's rows
     const char* b;                        // operand of the result's columns
-    const uint8_t* a_scales;              // kMx4
-    const uint8_t* b_scales;
+    const uint8_t* a_scales;              // kMx4; kInt8: fp32, one of each row of `a`, [rows],
+    const uint8_t* b_scales;              // and of `b`, [experts][width]
     char* out;
     const long long* ends;                // null: one group
     long long a_stride, b_stride;         // bytes from one row of the operand, as it lies, to the next
@@ -67,6 +67,7 @@ struct RawRows {
     long long stride;                     // elements
     float norm;                           // 1 / sqrt(2^log)
     int log;                              // runs of 2^log coordinates; 0: no rotation
+    int k;                                // kInt8: numbers of a row (the weights' rows are longer by what makes whole pieces)
 };
 constexpr int kRawChunks = 8;             // chunks of 512 numbers that a workgroup's eight waves quantise, one each
 // whether a group's rows are so few that every workgroup of the product does

@@ -1,9 +1,11 @@
 // Matrix products of grouped rows on the matrix pipe: tiles through LDS, and the form for a few rows.
 //
 // In every product a wave multiplies 32 rows by 32 columns over a depth of 32 bytes an instruction: 16 numbers of 16 bits
-// (v_mfma_f32_32x32x16) or 64 of 4 bits (v_mfma_scale_f32_32x32x64, e2m1 with an e8m0 scale for each 32), 16 bytes a lane from
-// either operand.  So one kernel moves bytes for all types, and what differs is the instruction and the scales.
+// (v_mfma_f32_32x32x16), 32 whole numbers of 8 (v_mfma_i32_32x32x32, sums of 32 bits) or 64 of 4 bits (v_mfma_scale_f32_32x32x64, e2m1 with
+// an e8m0 scale for each 32), 16 bytes a lane from either operand.  So one kernel moves bytes for all types, and what differs is the
+// instruction, the scales and, for whole numbers, the sums' type.
 #pragma once
+#include "int_lane.hpp"
 #include "mx4_lane.hpp"
 
 namespace spinner {
@@ -11,6 +13,7 @@ namespace spinner {
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef int intx16 __attribute__((ext_vector_type(16)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -110,10 +113,13 @@ __device__ __forceinline__ bool xcd_run(unsigned block, unsigned total, unsigned
 }
 
 // ------------------------------------------------------------------ one instruction
+template <int TYPE> using Sums16 = std::conditional_t<TYPE == kInt8, intx16, floatx16>;
+template <int TYPE> using Sums4 = std::conditional_t<TYPE == kInt8, intx4, floatx4>;
 template <int TYPE>
-__device__ __forceinline__ floatx16 multiply32(uintx4 a, uintx4 b, floatx16 c)
+__device__ __forceinline__ Sums16<TYPE> multiply32(uintx4 a, uintx4 b, Sums16<TYPE> c)
 {
-    if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    if constexpr (TYPE == kInt8) return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, a), __builtin_bit_cast(intx4, b), c, 0, 0, 0);
+    else if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ intx8 fp4_operand(uintx4 a)
@@ -127,9 +133,10 @@ __device__ __forceinline__ floatx16 multiply32_scaled(uintx4 a, uintx4 b, floatx
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(a), fp4_operand(b), c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
 }
 template <int TYPE>
-__device__ __forceinline__ floatx4 multiply16(uintx4 a, uintx4 b, floatx4 c)
+__device__ __forceinline__ Sums4<TYPE> multiply16(uintx4 a, uintx4 b, Sums4<TYPE> c)
 {
-    if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    if constexpr (TYPE == kInt8) return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, a), __builtin_bit_cast(intx4, b), c, 0, 0, 0);
+    else if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ floatx4 multiply16_scaled(uintx4 a, uintx4 b, floatx4 c, unsigned sa, unsigned sb)
@@ -370,7 +377,7 @@ product_kernel(ProductParams p)
 {
     static_assert(STAGES == 2 || !ANY, "loads through registers are one chunk ahead");
     constexpr int WAVES = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr bool MX = TYPE == kMx4;
+    constexpr bool MX = TYPE == kMx4, INT = TYPE == kInt8;
     // scales: two chunks' at a time, brought through registers a pair of chunks ahead; 64 x 64, where a wait for those would be one for
     // all chunks on their way, all of the depth's at the start
     constexpr bool HELD = MX && TM * TN == 1;
@@ -389,6 +396,7 @@ product_kernel(ProductParams p)
     int rows_left, cols_left, depth;          // depth: bytes (kForward, kDx: of A's rows), rows (kDw)
     Out* out = reinterpret_cast<Out*>(p.out);
     const uint8_t *a_scales = nullptr, *b_scales = nullptr;
+    const float *a_factors = nullptr, *b_factors = nullptr;
     unsigned a_end = 0, b_end = 0;            // scales from the tile's first to the operand's last
     if constexpr (DIRECTION == kDw) {
         // an equal share of every expert's tiles to each XCD: the depth of an expert's sums is the number of its rows
@@ -429,8 +437,12 @@ product_kernel(ProductParams p)
         b = p.b + (nobody ? 0 : at.expert) * p.b_group + (DIRECTION == kForward ? n0 * p.b_stride : n0 * 2LL);
         rows_left = at.hi - at.lo;
         cols_left = p.width - n0;
-        depth = nobody ? 0 : (MX ? p.depth / 2 : p.depth * 2);
+        depth = nobody ? 0 : (MX ? p.depth / 2 : INT ? p.depth : p.depth * 2);
         out += at.lo * p.out_stride + n0;
+        if constexpr (INT) {
+            a_factors = nobody ? nullptr : reinterpret_cast<const float*>(p.a_scales) + at.lo;
+            b_factors = reinterpret_cast<const float*>(p.b_scales) + (nobody ? 0 : at.expert) * (long long)p.width + n0;
+        }
         if constexpr (MX) {
             const long long count = p.depth / kMx4Block;
             const long long from_a = at.lo * count, from_b = ((nobody ? 0 : at.expert) * (long long)p.width + n0) * count;
@@ -447,13 +459,13 @@ product_kernel(ProductParams p)
     B ob;
     oa.start(p.a_stride, rows_left, wave, lane);
     ob.start(p.b_stride, cols_left, wave, lane);
-    floatx16 acc[TM][TN];
+    Sums16<TYPE> acc[TM][TN];
 #pragma unroll
     for (int t = 0; t < TM; ++t)
 #pragma unroll
         for (int u = 0; u < TN; ++u)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[t][u][v] = 0.0f;
+            for (int v = 0; v < 16; ++v) acc[t][u][v] = 0;
 
     // depth in units of an operand: bytes along deep rows, rows of flat ones
     constexpr int unit_a = DIRECTION == kDw ? kChunkDepth16 : kChunkBytes, unit_b = DIRECTION == kForward ? kChunkBytes : kChunkDepth16;
@@ -613,7 +625,7 @@ product_kernel(ProductParams p)
         // sums meet at the end.
         static_assert(BM == 64 && BN == 64 && WAVES == 4, "a quarter of the result a wave");
         uintx4 fa[2][2], fb[2][2];
-        floatx16 sum[2][2];
+        Sums16<TYPE> sum[2][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -676,21 +688,22 @@ product_kernel(ProductParams p)
             chunk(c + 1, s1);
         }
         meet(s0);
-        floatx4* part = reinterpret_cast<floatx4*>(buffers);
+        using Four = Sums4<TYPE>;
+        Four* part = reinterpret_cast<Four*>(buffers);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    part[((wave * 4 + t * 2 + u) * 4 + q) * 64 + lane] = floatx4{sum[t][u][4 * q], sum[t][u][4 * q + 1], sum[t][u][4 * q + 2], sum[t][u][4 * q + 3]};
+                    part[((wave * 4 + t * 2 + u) * 4 + q) * 64 + lane] = Four{sum[t][u][4 * q], sum[t][u][4 * q + 1], sum[t][u][4 * q + 2], sum[t][u][4 * q + 3]};
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            floatx4 v[4];
+            Four v[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) v[w] = part[((w * 4 + wave) * 4 + q) * 64 + lane];
-            const floatx4 all = (v[0] + v[1]) + (v[2] + v[3]);
+            const Four all = (v[0] + v[1]) + (v[2] + v[3]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[0][0][4 * q + k] = all[k];
         }
@@ -703,6 +716,27 @@ product_kernel(ProductParams p)
     constexpr int kOutPieces = TN * 32 * (int)sizeof(Out) / 16, kPieceOuts = 16 / (int)sizeof(Out);
     static_assert(WAVES * 32 * kOutPieces <= STAGES * kBuffer, "fits the buffers");
     uintx4* mine = buffers + wave * 32 * kOutPieces;
+    // whole numbers: an exact sum, rounded to fp32 once, times the column's factor and then the row's, in its place
+    if constexpr (INT) {
+        float by_row[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            const int row = (wm * TM + t) * 32 + (lane & 31);
+            by_row[t] = a_factors ? a_factors[row < m_rows ? row : m_rows - 1] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < TN; ++u)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int col = (wn * TN + u) * 32 + 8 * q + 4 * (lane >> 5);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float by_column = a_factors ? b_factors[col + k < cols_left ? col + k : cols_left - 1] : 0.0f;
+#pragma unroll
+                    for (int t = 0; t < TM; ++t) acc[t][u][4 * q + k] = a_factors ? __float_as_int((float)acc[t][u][4 * q + k] * by_column * by_row[t]) : 0;
+                }
+            }
+    }
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
 #pragma unroll
@@ -746,13 +780,16 @@ struct Run {
 template <int TYPE, int NT, typename Out, bool RAW>
 __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductParams p, unsigned columns, RawRows raw)
 {
-    constexpr bool MX = TYPE == kMx4;
-    static_assert(MX || !RAW, "rows are quantised for 4-bit weights");
+    constexpr bool MX = TYPE == kMx4, INT = TYPE == kInt8;
+    static_assert(MX || INT || !RAW, "rows are quantised for weights of 4 and 8 bits");
+    constexpr int kCodePieces = INT ? 32 : 16;                        // of 16 bytes, a chunk of 512 codes
     __shared__ float4 meeting[RAW ? kRawChunks * 128 : 1];
-    __shared__ uintx4 own_codes[RAW ? kRawChunks * 16 : 1], own_scales[RAW ? kRawChunks : 1];
+    __shared__ uintx4 own_codes[RAW ? kRawChunks * kCodePieces : 1], own_scales[RAW && MX ? kRawChunks : 1];
+    __shared__ int largest[RAW && INT ? kRawChunks : 1];
     // waves share the depth by four; RAW: and the columns by two, so that eight waves quantise
     constexpr int PARTS = RAW ? 2 : 1;
-    __shared__ floatx4 part[4 * PARTS][NT][64];
+    using Four = Sums4<TYPE>;
+    __shared__ Four part[4 * PARTS][NT][64];
     const int lane = threadIdx.x & 63, in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_group & 3;
     const int r16 = lane & 15, quarter = lane >> 4;
     RowTiles<16> tiles(p);
@@ -762,11 +799,11 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
     const int n0 = tile % columns * (16 * NT * PARTS);
     const bool nobody = at.expert == p.experts;
     const int rows_left = at.hi - at.lo;
-    const int bytes = nobody ? 0 : (MX ? p.depth / 2 : p.depth * 2);
+    const int bytes = nobody ? 0 : (MX ? p.depth / 2 : INT ? p.depth : p.depth * 2);
     const int row_scales = p.depth / kMx4Block;
     const int row = at.lo + (r16 < rows_left ? r16 : rows_left - 1);
     const int row_chunks = (p.depth + kChunk - 1) / kChunk;           // RAW: a row in LDS is so many whole chunks
-    const char *x = RAW ? reinterpret_cast<const char*>(own_codes) + (row - at.lo) * row_chunks * 256 + quarter * 16 : p.a + row * p.a_stride + quarter * 16, *w[NT];
+    const char *x = RAW ? reinterpret_cast<const char*>(own_codes) + (row - at.lo) * row_chunks * (kCodePieces * 16) + quarter * 16 : p.a + row * p.a_stride + quarter * 16, *w[NT];
     const uint8_t *xs = !MX ? nullptr : RAW ? reinterpret_cast<const uint8_t*>(own_scales) + (row - at.lo) * row_chunks * 16 : p.a_scales + (long long)row * row_scales, *ws[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -774,9 +811,9 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
         w[t] = p.b + (nobody ? 0 : at.expert) * p.b_group + n * p.b_stride + quarter * 16;
         ws[t] = MX ? p.b_scales + ((nobody ? 0 : at.expert) * (long long)p.width + n) * row_scales : nullptr;
     }
-    floatx4 acc[NT];
+    Four acc[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = floatx4{0, 0, 0, 0};
+    for (int t = 0; t < NT; ++t) acc[t] = Four{0, 0, 0, 0};
 
     const auto piece16 = [](const void* from) {
         struct __attribute__((packed, aligned(1))) Sixteen { unsigned v[4]; };
@@ -787,7 +824,7 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
     const auto take = [&](Run<TYPE, NT>& run, int k) {
 #pragma unroll
         for (int i = 0; i < kRunSteps; ++i) run.x[i] = RAW ? *reinterpret_cast<const uintx4*>(x + (k * kRunSteps + i) * 64) : fetch_whole(x + (k * kRunSteps + i) * 64);
-        if constexpr (RAW) run.xs = *reinterpret_cast<const uintx4*>(xs + k * kRunSteps * 4);
+        if constexpr (RAW && MX) run.xs = *reinterpret_cast<const uintx4*>(xs + k * kRunSteps * 4);
         else if constexpr (MX) run.xs = piece16(xs + k * kRunSteps * 4);
     };
     const auto fetch = [&](Run<TYPE, NT>& run, int k) {
@@ -817,11 +854,12 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
         using Lane = LaneNumbers<Out>;
         const int chunks = nobody ? 0 : (rows_left < 16 ? rows_left : 16) * row_chunks, c = in_group, r = c / row_chunks, in_row = c - r * row_chunks;
         const unsigned flip = raw.log > 0 ? Lane::flip(raw.log, lane) : 0;
-        const Lane l(in_row, lane, p.depth);
+        const Lane l(in_row, lane, INT ? raw.k : p.depth);
         Quad quads[Lane::HALVES];
         float d[kPieceNumbers], v[kPieceNumbers];
         if (c < chunks) {
-            l.fetch(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride);
+            if constexpr (INT) fetch_chunk<Out>(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride, l.first, raw.k);
+            else l.fetch(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride);
             if (raw.log > 0) l.diagonal(d, raw.diag, raw.norm);
         }
         if (k < runs) fetch(now, k);
@@ -831,11 +869,30 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
             if (raw.log > 9) Lane::meet(v, meeting + c * 128, lane);
         }
         if (raw.log > 9) __syncthreads();
-        if (c < chunks) {
-            if (raw.log > 9) {
-                const int own = in_row & (waves_of_run(raw.log) - 1);
-                Lane::join(v, meeting + (c - own) * 128, waves_of_run(raw.log), own, lane);
+        if (c < chunks && raw.log > 9) {
+            const int own = in_row & (waves_of_run(raw.log) - 1);
+            Lane::join(v, meeting + (c - own) * 128, waves_of_run(raw.log), own, lane);
+        }
+        if constexpr (INT) {
+            if (c < chunks) {
+                const int top = wave_largest(largest_bits(v, 0));
+                if (lane == 0) largest[c] = top;
             }
+            __syncthreads();
+            if (c < chunks) {
+                int top = 0;
+                for (int w = 0; w < row_chunks; ++w) top = largest[c - in_row + w] > top ? largest[c - in_row + w] : top;
+                const RowScale s(top);
+                const float factor = flip ? -s.factor : s.factor;
+                unsigned code[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) code[i] = s.bad ? 0u : raw.log > 0 ? four_codes<false>(v + 4 * i, factor, 0.0f) : four_codes<true>(v + 4 * i, factor, s.scale);
+                unsigned* to = reinterpret_cast<unsigned*>(own_codes) + c * kCodePieces * 4;
+                if constexpr (Lane::HALVES == 1) *reinterpret_cast<uint2*>(to + lane * 2) = uint2{code[0], code[1]};
+                else { to[lane] = code[0]; to[64 + lane] = code[1]; }
+            }
+        }
+        if (MX && c < chunks) {
             unsigned codes;
             int byte[Lane::HALVES];
             const int col = l.encode(v, flip, lane, &codes, byte), start = in_row * kChunk;
@@ -858,7 +915,7 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
     if (k < runs) multiply(now, k);
     // what is left is less than a run: a step a wave
     if (const int s = runs * kRunSteps + wave; s * 64 < bytes) {
-        const int count = (bytes - s * 64 - quarter * 16) >> 1;        // 16-bit numbers, or pairs of codes
+        const int count = (bytes - s * 64 - quarter * 16) >> 1;        // 16-bit numbers, or pairs of bytes
         uintx4 fw[NT], fx;
         unsigned sw[NT], sx = 0x7f;
         if (!MX && bytes < 16) {
@@ -896,7 +953,26 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
     const bool vector = p.out_stride % 4 == 0;
     if (in_group < NT * PARTS && r16 < rows_left) {
         const int first = in_group / NT * 4, t = in_group % NT, col = n0 + in_group * 16 + 4 * quarter;
-        const floatx4 sum = (part[first][t][lane] + part[first + 1][t][lane]) + (part[first + 2][t][lane] + part[first + 3][t][lane]);
+        const Four whole = (part[first][t][lane] + part[first + 1][t][lane]) + (part[first + 2][t][lane] + part[first + 3][t][lane]);
+        floatx4 sum;
+        if constexpr (INT) {
+            float by_row = 0.0f;
+            if constexpr (RAW) {
+                int top = 0;
+                if (!nobody)
+                    for (int w = 0; w < row_chunks; ++w) top = largest[r16 * row_chunks + w] > top ? largest[r16 * row_chunks + w] : top;
+                by_row = RowScale(top).scale;
+            } else {
+                by_row = nobody ? 0.0f : reinterpret_cast<const float*>(p.a_scales)[row];
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int own = col + v < p.width ? col + v : p.width - 1;
+                sum[v] = nobody ? 0.0f : (float)whole[v] * reinterpret_cast<const float*>(p.b_scales)[at.expert * (long long)p.width + own] * by_row;
+            }
+        } else {
+            sum = whole;
+        }
         Out* out = reinterpret_cast<Out*>(p.out) + (at.lo + r16) * p.out_stride + col;
         store_four(out, sum[0], sum[1], sum[2], sum[3], p.width - col, vector);
     }
@@ -996,7 +1072,7 @@ constexpr long long kFarthestRow = 1 << 23;
 template <int DIRECTION, int TYPE>
 bool whole_pieces(const ProductParams& p)
 {
-    if (TYPE == kMx4) return true;                                    // rows of 16 bytes for each 32 numbers, at most 2^23 bytes
+    if (TYPE == kMx4 || TYPE == kInt8) return true;                   // rows of whole pieces of 16 bytes, at most 2^23 bytes
     if (p.a_stride > kFarthestRow || p.b_stride > kFarthestRow) return false;
     const int a_row = DIRECTION == kDw ? p.height : p.depth;
     const int b_row = DIRECTION == kForward ? p.depth : p.width;
@@ -1028,7 +1104,9 @@ hipError_t launch_product_as(const ProductParams& p, hipStream_t s)
 {
     if constexpr (DIRECTION == kForward)
         if (p.tile == kFewRows) return launch_few_rows_as<TYPE, Out, false>(p, RawRows{}, s);
-    if constexpr (TYPE != kMx4) {
+    if constexpr (TYPE == kInt8)
+        if (p.tile == kTile128Deep) return launch_tiles<DIRECTION, TYPE, 128, 128, 4, false, Out>(p, s);
+    if constexpr (TYPE != kMx4 && TYPE != kInt8) {
         // (the same order of the sums as with whole pieces: each number's in the order of the depth, or a quarter of each chunk a wave.)  y, dx, dw in us beside the next sizes of whole
         // pieces: 16384 x 4095 x 4097 837, 871, 1200 for 411, 419, 432; 20000 x 301 x 403, 16 experts 27, 23, 127 for 17, 12, 45; 24 x 4095 x 2047, 8 experts (y: few rows) 62, 44, 80 for 21, 25, 53
         if (!whole_pieces<DIRECTION, TYPE>(p))

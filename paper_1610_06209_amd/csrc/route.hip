@@ -1,0 +1,728 @@
+// A router's logits to experts and weights, with the gradient, and the chosen experts to places in their order.
+#include <math.h>
+
+#include "mx4.hpp"
+#include "number_io.hpp"
+#include "route.hpp"
+#include "spinner_kernels.hpp"
+
+namespace spinner {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr long long kRouteBlocks = 1 << 20;          // most workgroups: a grid holds fewer than 2^32 threads, and goes down the rows
+
+// v of the lane that takes turns with this one in a join over 2 MASK lanes, when lanes of MASK have joined before: mirrored rows for 4 and 8, which the
+// adders read in place
+template <int MASK>
+__device__ __forceinline__ int across(int v)
+{
+    if constexpr (MASK == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);        // row_half_mirror
+    else if constexpr (MASK == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);   // row_mirror
+    else return lane_xor_i<MASK>(v);
+}
+template <int MASK> __device__ __forceinline__ unsigned across(unsigned v) { return (unsigned)across<MASK>((int)v); }
+template <int MASK> __device__ __forceinline__ float across(float v) { return __int_as_float(across<MASK>(__float_as_int(v))); }
+template <int MASK> __device__ __forceinline__ double across(double v) { return __hiloint2double(across<MASK>(__double2hiint(v)), across<MASK>(__double2loint(v))); }
+
+// ------------------------------------------------------------------ lanes of a row
+// `op` over a row's LANES lanes (16: a row of the instruction set's own, joined in its registers), in all of them
+template <int LANES, typename V, typename F>
+__device__ __forceinline__ V join_lanes(V v, F op)
+{
+    v = op(v, across<1>(v));
+    v = op(v, across<2>(v));
+    v = op(v, across<4>(v));
+    v = op(v, across<8>(v));
+    if constexpr (LANES == 64) {
+        v = op(v, across<16>(v));
+        v = op(v, across<32>(v));
+    }
+    return v;
+}
+struct Sum { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; } };
+struct Larger { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a > b ? a : b; } };
+template <int LANES>
+__device__ __forceinline__ bool any_lane(bool v)
+{
+    const unsigned long long all = __ballot(v);
+    if constexpr (LANES == 64) return all != 0;
+    return (all >> (threadIdx.x & 48) & 0xffff) != 0;
+}
+
+// What the wave's lanes have written to LDS, in order, is there for all of them: the LDS keeps the order of a wave, and so has the compiler to.
+__device__ __forceinline__ void wave_meets()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// exp(x) for x <= 0 to 2^-22 of itself: 2^h with the product's remainder put back (x log2(e) alone would be off by |x| 2^-24); 0 from -87 down
+__device__ __forceinline__ float exp_below(float x)
+{
+    x = fmaxf(x, -200.0f);
+    const float h = x * 1.44269502f, l = __builtin_fmaf(x, 1.44269502f, -h) + x * 1.92596303e-8f;
+    return __builtin_amdgcn_exp2f(h) * __builtin_fmaf(l, 0.693147182f, 1.0f);
+}
+__device__ __forceinline__ float sigmoid(float l)
+{
+    const float e = exp_below(-__builtin_fabsf(l));
+    return (l > 0.0f ? 1.0f : e) / (1.0f + e);
+}
+
+// Which experts a lane has: of LANES / 2^log_groups lanes each group, `mine` neighbours from `first` on, at most R.
+struct Share {
+    int group, first, mine;
+    __device__ __forceinline__ Share(int lane, int lanes, int log_groups, int groups, int size)
+    {
+        const int each = lanes >> log_groups, in_group = lane & (each - 1), part = (size + each - 1) / each;
+        group = lane / each;
+        first = group * size + in_group * part;
+        const int left = size - in_group * part;
+        mine = group < groups ? (left < part ? left : part) : 0;
+    }
+};
+
+// a lane's logits, those that it has none of -inf
+template <typename T, int R>
+__device__ __forceinline__ void load_logits(float (&v)[R], const T* row, int first, int mine, int count)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    if (R % N == 0 && first + R <= count) {
+#pragma unroll
+        for (int i = 0; i < R / N; ++i) {
+            const auto q = *reinterpret_cast<const typename LooseQuad<sizeof(T)>::type*>(row + first + i * N);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                float f;
+                if constexpr (sizeof(T) == 4) f = __uint_as_float(q[k]);
+                else f = (float)__builtin_bit_cast(typename Pair16<T>::Pair, (unsigned)q[k >> 1])[k & 1];
+                v[i * N + k] = i * N + k < mine ? f : -INFINITY;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) v[r] = r < mine ? (float)row[first + r] : -INFINITY;
+    }
+}
+
+// a number's bits in the order of the numbers, as unsigned whole numbers (-0 is 0)
+__device__ __forceinline__ unsigned ordered(float v)
+{
+    const int b = __float_as_int(v + 0.0f);
+    return (unsigned)b ^ ((unsigned)(b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float number_of(unsigned u)
+{
+    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
+// weight of a chosen logit without the factor that all share: softmax exp(l - top), sigmoid 1 / (1 + exp(-l)) over exp(top), top the largest
+// min(l, 0), so that the largest is at least a half and their sum is no 0
+template <int SCORE>
+__device__ __forceinline__ float share_of(float logit, float top)
+{
+    if constexpr (SCORE == kSoftmax) return exp_below(logit - top);
+    return exp_below(fminf(logit, 0.0f) - top) / (1.0f + exp_below(-__builtin_fabsf(logit)));
+}
+
+// The two largest of a group's keys, of its `each` lanes
+template <typename V>
+struct Two {
+    V a, b;
+    __device__ __forceinline__ void take(V k)
+    {
+        const V low = a < k ? a : k;
+        b = b > low ? b : low;
+        a = a > k ? a : k;
+    }
+    __device__ __forceinline__ void merge(V a2, V b2)
+    {
+        const V low = a < a2 ? a : a2, high = b > b2 ? b : b2;
+        b = low > high ? low : high;
+        a = a > a2 ? a : a2;
+    }
+    __device__ __forceinline__ void lanes(int each)
+    {
+        if (each > 1) merge(across<1>(a), across<1>(b));
+        if (each > 2) merge(across<2>(a), across<2>(b));
+        if (each > 4) merge(across<4>(a), across<4>(b));
+        if (each > 8) merge(across<8>(a), across<8>(b));
+        if (each > 16) merge(across<16>(a), across<16>(b));
+        if (each > 32) merge(across<32>(a), across<32>(b));
+    }
+};
+
+constexpr double kNever = -(double)INFINITY;
+constexpr int kCandidates = 48;                       // of a row, at most: its choices and what may lie level with the last of them
+constexpr float kNear = 4e-6f;                        // keys that lie nearer, in units of themselves and of the largest bias, may be the other way round
+
+// What decides, in fp64, from the row's logits in LDS: the groups that stay, and the choices, each the largest key behind the one before.  For rows
+// whose keys are too near each other in fp32; keys are made again for each choice, which few rows pay for and no register.
+template <int LANES, int R, int SCORE>
+__device__ __forceinline__ void choose64(const RouteParams& p, const float* logits, const Share& at, float top, int lane, double* group_keys, int* chosen)
+{
+    const float* l = logits + lane * R;
+    double sum = 0.0;
+    if constexpr (SCORE == kSoftmax) {
+#pragma unroll 1
+        for (int r = 0; r < at.mine; ++r) sum += l[r] > -INFINITY ? exp((double)l[r] - (double)top) : 0.0;
+        sum = join_lanes<LANES>(sum, Sum{});
+    }
+    const auto score = [&](int r) {
+        const double s = SCORE == kSoftmax ? exp((double)l[r] - (double)top) / sum : 1.0 / (1.0 + exp(-(double)l[r]));
+        return l[r] > -INFINITY ? s + (p.bias ? (double)p.bias[at.first + r] : 0.0) : kNever;
+    };
+    bool stays = true;
+    if (p.groups > 1) {
+        const int each = LANES >> p.log_groups;
+        Two<double> two = {kNever, kNever};
+#pragma unroll 1
+        for (int r = 0; r < at.mine; ++r) two.take(p.bias || p.group_top > 1 ? score(r) : (double)l[r]);
+        two.lanes(each);
+        const double own = p.group_top > 1 && two.b > kNever ? two.a + two.b : two.a;
+        if ((lane & (each - 1)) == 0) group_keys[at.group] = own;
+        wave_meets();
+        int larger = 0;
+        for (int g = 0; g < p.groups; ++g) {
+            const double other = group_keys[g];
+            larger += (other > own) | ((other == own) & (g < at.group)) ? 1 : 0;
+        }
+        stays = larger < p.top_groups;
+        wave_meets();
+    }
+    double last = (double)INFINITY;
+    int last_at = -1;
+    for (int j = 0; j < p.top; ++j) {
+        double v = kNever;
+        int which = 0x7fffffff;
+#pragma unroll 1
+        for (int r = 0; r < at.mine; ++r) {
+            const double k = p.bias ? score(r) : (double)l[r];
+            const int own = at.first + r;
+            const bool behind = (k < last) | ((k == last) & (own > last_at));
+            const bool other = stays & behind & (k > v);
+            v = other ? k : v;
+            which = other ? own : which;
+        }
+        last = join_lanes<LANES>(v, Larger{});
+        last_at = join_lanes<LANES>(v == last ? which : 0x7fffffff, [](int a, int b) { return a < b ? a : b; });
+        if (lane == 0) chosen[j] = last > kNever ? last_at : -1;
+    }
+    wave_meets();
+}
+
+// LANES lanes a row, up to R neighbouring experts each, in registers from the logits to the choice.
+// A candidate is the largest of whole numbers of 32 bits below the last one: the first 22 of the key's bits in the order of the numbers, and 10 that put
+// equal ones in the order of their index.  EXACT (16-bit logits, no bias: the key is the logit, of which 22 bits are all there is): the candidates
+// are the choices.  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32;
+// rows with neighbours, or groups at the border, that fp32 does not tell apart (and that are not equal by having the same logit and bias) are
+// taken again by choose64.
+template <typename T, int LANES, int R, int SCORE, bool EXACT>
+__global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
+{
+    constexpr int ROWS = kThreads / LANES, HELD = (kMostChosen + LANES - 1) / LANES, HELD_ALL = (kCandidates + LANES - 1) / LANES;
+    constexpr unsigned kLow = 1023;
+    __shared__ float logits[ROWS][LANES * R];
+    __shared__ double group_keys[ROWS][kMostRouteGroups];
+    __shared__ unsigned order[ROWS][kCandidates];
+    __shared__ float keys_of[EXACT ? 1 : ROWS][EXACT ? 1 : kCandidates];
+    __shared__ int chosen[ROWS][kMostChosen];
+    const int lane = threadIdx.x & (LANES - 1), slot = threadIdx.x / LANES, size = p.count / p.groups;
+    const Share at(lane, LANES, p.log_groups, p.groups, size);
+    const int each = LANES >> p.log_groups, part_of = (size + each - 1) / each;
+    // where an expert's logit lies in LDS
+    const auto place = [&](int w) {
+        const int g = w / size, in_group = w - g * size, l = in_group / part_of;
+        return (g * each + l) * R + in_group - l * part_of;
+    };
+    float bias[R], largest_bias = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) bias[r] = 0.0f;
+    if (!EXACT && p.bias) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            bias[r] = p.bias[r < at.mine ? at.first + r : 0];
+            bias[r] = r < at.mine ? bias[r] : 0.0f;
+            // (infinities are far from all others)
+            largest_bias = fmaxf(largest_bias, __builtin_fabsf(bias[r]) < INFINITY ? __builtin_fabsf(bias[r]) : 0.0f);
+        }
+        largest_bias = join_lanes<LANES>(largest_bias, Larger{});
+    }
+    const auto reach = [&](float key) { return kNear * (__builtin_fabsf(key) + 2.0f * largest_bias); };
+    for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
+        const long long own = r0 + slot, row = own < p.rows ? own : p.rows - 1;
+        float l[R];
+        load_logits<T, R>(l, static_cast<const T*>(p.logits) + row * p.stride, at.first, at.mine, p.count);
+        const bool routed = !p.mask || p.mask[row] != 0;
+        bool bad = false;                  // a NaN, or an infinity in a softmax
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            bad |= (l[r] != l[r]) | (bias[r] != bias[r]) | (SCORE == kSoftmax && l[r] == INFINITY);
+            logits[slot][lane * R + r] = l[r];
+        }
+        bad = any_lane<LANES>(bad);
+        float top = -INFINITY, sum = 0.0f;
+        const bool scored = (!EXACT && p.bias) || p.group_top > 1;
+        float key[R];
+        if (SCORE == kSoftmax && (scored || !p.renormalise)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) top = fmaxf(top, l[r]);
+            top = join_lanes<LANES>(top, Larger{});
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                key[r] = exp_below(l[r] - top);
+                sum += key[r];
+            }
+            sum = join_lanes<LANES>(sum, Sum{});
+        }
+        // keys, -inf for what cannot be chosen
+        const float part = 1.0f / sum;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (scored) {
+                const float s = SCORE == kSoftmax ? key[r] * part : sigmoid(l[r]);
+                key[r] = l[r] > -INFINITY ? s + bias[r] : -INFINITY;
+            } else {
+                key[r] = l[r];
+            }
+        }
+        bool near = false, stays = true;
+        if (p.groups > 1) {
+            Two<float> two = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int r = 0; r < R; ++r) two.take(key[r]);
+            two.lanes(each);
+            const float mine = p.group_top > 1 && two.b > -INFINITY ? two.a + two.b : two.a;
+            float* keys = reinterpret_cast<float*>(group_keys[slot]);
+            if ((lane & (each - 1)) == 0) keys[at.group] = mine;
+            wave_meets();
+            int larger = 0;
+            float below = -INFINITY;       // the largest of the keys that come after this one
+            for (int g = 0; g < p.groups; ++g) {
+                const float other = keys[g];
+                const bool first = (other > mine) | ((other == mine) & (g < at.group));
+                larger += first ? 1 : 0;
+                below = (first | (g == at.group)) ? below : fmaxf(below, other);
+            }
+            stays = larger < p.top_groups;
+            // the border lies behind the last group that stays
+            near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) & (mine - below <= reach(mine));
+            wave_meets();
+        }
+        unsigned k[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float v = EXACT || !p.bias ? l[r] : key[r];
+            k[r] = stays && v > -INFINITY ? (ordered(v) & ~kLow) | (kLow - (at.first + r)) : 0;
+        }
+        // the largest number below the last one, which leaves it the largest of the differences to that, modulo 2^32
+        unsigned last = 0xffffffffu;
+        float border = 0.0f;
+        bool open = !EXACT;                // whether there may be more candidates for the last choice
+        int count = 0;
+        for (;;) {
+            unsigned best = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const unsigned t = k[r] - last;
+                best = t > best ? t : best;
+            }
+            const unsigned next = join_lanes<LANES>(best, Larger{}) + last;
+            last = next < last ? next : 0;
+            if (lane == 0) order[slot][count] = last;
+            ++count;
+            if constexpr (EXACT) {
+                if (count == p.top) break;
+            } else if (count >= p.top) {
+                // (22 bits: off by 2^-13 of the number, or 2^-139)
+                const float v = number_of(last & ~kLow);
+                if (count == p.top) border = v;
+                else open = open & (last != 0) & (border - v <= reach(border) + 5e-4f * __builtin_fabsf(border) + 1e-40f);
+                if (count > p.top && __ballot(open) == 0) break;
+                if (count == kCandidates) break;
+            }
+        }
+        wave_meets();
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                const int j = h * LANES + lane;
+                if (j < p.top) chosen[slot][j] = order[slot][j] ? (int)(kLow - (order[slot][j] & kLow)) : -1;
+            }
+        } else {
+            near |= open;
+            float v[HELD_ALL];
+            int index[HELD_ALL], rank[HELD_ALL];
+#pragma unroll
+            for (int h = 0; h < HELD_ALL; ++h) {
+                const int j = h * LANES + lane;
+                v[h] = -INFINITY;
+                index[h] = 0x7fffffff;
+                rank[h] = 0;
+                if (j < count && order[slot][j]) {
+                    index[h] = (int)(kLow - (order[slot][j] & kLow));
+                    const float x = logits[slot][place(index[h])];
+                    v[h] = !p.bias ? x : (SCORE == kSoftmax ? exp_below(x - top) * part : sigmoid(x)) + p.bias[index[h]];
+                }
+                if (j < count) keys_of[slot][j] = v[h];
+            }
+            wave_meets();
+            for (int i = 0; i < count; ++i) {
+                const float other = keys_of[slot][i];
+                const int other_index = (int)(kLow - (order[slot][i] & kLow));
+#pragma unroll
+                for (int h = 0; h < HELD_ALL; ++h) {
+                    if (h * LANES >= count) break;
+                    const bool first = (other > v[h]) | ((other == v[h]) & (other_index < index[h]));
+                    rank[h] += first ? 1 : 0;
+                    // logits without a bias are the keys; else equal logits with equal biases are equal
+                    if (p.bias && (order[slot][i] != 0) & (v[h] > -INFINITY) & (other_index != index[h]) & (__builtin_fabsf(other - v[h]) <= reach(other)))
+                        near |= (logits[slot][place(other_index)] != logits[slot][place(index[h])]) | (p.bias[other_index] != p.bias[index[h]]);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < HELD; ++h)
+                if (h * LANES + lane < p.top) chosen[slot][h * LANES + lane] = -1;
+            wave_meets();
+#pragma unroll
+            for (int h = 0; h < HELD_ALL; ++h)
+                if (v[h] > -INFINITY && rank[h] < p.top) chosen[slot][rank[h]] = index[h];
+        }
+        near = any_lane<LANES>(near);
+        if (__builtin_expect(__ballot(near) != 0, 0)) {
+            __shared__ int again[ROWS][kMostChosen];
+            float highest = -INFINITY;
+            if constexpr (SCORE == kSoftmax) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) highest = fmaxf(highest, l[r]);
+                highest = join_lanes<LANES>(highest, Larger{});
+            }
+            choose64<LANES, R, SCORE>(p, logits[slot], at, highest, lane, group_keys[slot], again[slot]);
+            if (near)
+                for (int j = lane; j < p.top; j += LANES) chosen[slot][j] = again[slot][j];
+        }
+        wave_meets();
+        // weights: choice j is lane j mod LANES's
+        int which[HELD];
+        float value[HELD], own_top = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            const int j = h * LANES + lane;
+            which[h] = j < p.top ? chosen[slot][j] : -1;
+            value[h] = which[h] < 0 ? -INFINITY : logits[slot][place(which[h] < 0 ? 0 : which[h])];
+            own_top = fmaxf(own_top, SCORE == kSigmoid ? fminf(value[h], 0.0f) : value[h]);
+        }
+        float factor = p.scale;
+        if (p.renormalise) {
+            top = join_lanes<LANES>(own_top, Larger{});
+            sum = 0.0f;
+        } else if (SCORE == kSigmoid) {
+            top = 0.0f;
+        }
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            value[h] = which[h] >= 0 ? share_of<SCORE>(value[h], top) : 0.0f;
+            if (p.renormalise) sum += value[h];
+        }
+        if (p.renormalise) sum = join_lanes<LANES>(sum, Sum{});
+        if (p.renormalise || SCORE == kSoftmax) factor = sum > 0.0f ? p.scale / sum : 0.0f;
+        if (own < p.rows) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                const int j = h * LANES + lane;
+                if (j < p.top) {
+                    p.experts[own * p.top + j] = routed && !bad ? which[h] : -1;
+                    p.weights[own * p.top + j] = !routed ? 0.0f : bad ? __builtin_nanf("") : value[h] * factor;
+                }
+            }
+        }
+        wave_meets();
+    }
+}
+
+// Gradient of the logits.  With p the scores of a row, w_j = scale p_j of the chosen ones gives
+//   softmax      dl_i = p_i (d_i - sum_j d_j p_j)          d_i = scale dw_i of a chosen one, 0 of others
+//   sigmoid      dl_i = d_i p_i (1 - p_i)
+// and w_j = scale q_j, q_j = p_j / (sum of the chosen ones'), on the chosen ones only
+//   softmax      dl_i = q_i (d_i - sum_j d_j q_j)          sigmoid: (1 - p_i) times that
+template <typename T, int LANES, int R, int SCORE>
+__global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
+{
+    constexpr int ROWS = kThreads / LANES, HELD = (kMostChosen + LANES - 1) / LANES;
+    __shared__ float spread[ROWS][LANES * R];
+    __shared__ float taken[ROWS][kMostChosen];
+    __shared__ int named[ROWS][kMostChosen];
+    const int lane = threadIdx.x & (LANES - 1), first = lane * R, slot = threadIdx.x / LANES;
+    const bool all = SCORE == kSoftmax && !p.renormalise;          // every logit has a gradient, not the chosen ones alone
+    for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
+        const long long own = r0 + slot, row = own < p.rows ? own : p.rows - 1;
+        const T* from = static_cast<const T*>(p.logits) + row * p.stride;
+        float e[R], top = -INFINITY, sum = 0.0f;
+        if (all) {
+            load_logits<T, R>(e, from, first, p.count - first, p.count);
+#pragma unroll
+            for (int r = 0; r < R; ++r) top = fmaxf(top, e[r]);
+            top = join_lanes<LANES>(top, Larger{});
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                e[r] = exp_below(e[r] - top);
+                sum += e[r];
+            }
+            sum = join_lanes<LANES>(sum, Sum{});
+        }
+        int at[HELD];
+        float d[HELD], value[HELD], share[HELD], own_top = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            const int j = h * LANES + lane;
+            at[h] = j < p.top ? p.experts[row * p.top + j] : -1;
+            at[h] = (unsigned)at[h] < (unsigned)p.count ? at[h] : -1;
+            d[h] = at[h] >= 0 ? p.scale * p.dweights[row * p.top + j] : 0.0f;
+            value[h] = at[h] >= 0 ? (float)from[at[h]] : -INFINITY;
+            own_top = fmaxf(own_top, SCORE == kSigmoid ? fminf(value[h], 0.0f) : value[h]);
+        }
+        if (p.renormalise) top = join_lanes<LANES>(own_top, Larger{});
+        else if (SCORE == kSigmoid) top = 0.0f;
+        float dot = 0.0f;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            share[h] = at[h] >= 0 ? share_of<SCORE>(value[h], top) : 0.0f;
+            if (p.renormalise) sum += share[h];
+        }
+        if (p.renormalise) sum = join_lanes<LANES>(sum, Sum{});
+        const float part = p.renormalise || SCORE == kSoftmax ? (sum > 0.0f ? 1.0f / sum : 0.0f) : 1.0f;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            share[h] *= part;
+            dot += d[h] * share[h];
+        }
+        dot = join_lanes<LANES>(dot, Sum{});
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            // (of the whole softmax: what a chosen one has beside the row's dot product)
+            d[h] = share[h] * (p.renormalise ? d[h] - dot : d[h]);
+            if (SCORE == kSigmoid) {                               // 1 - p
+                const float x = exp_below(-__builtin_fabsf(value[h]));
+                d[h] *= (value[h] > 0.0f ? x : 1.0f) / (1.0f + x);
+            }
+            const int j = h * LANES + lane;
+            if (j < p.top) { taken[slot][j] = at[h] >= 0 ? d[h] : 0.0f; named[slot][j] = at[h]; }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) spread[slot][first + r] = 0.0f;
+        wave_meets();
+        // an expert that a row names more than once: the sum, in the order of the choices, written by each of them
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            float total = 0.0f;
+            for (int j = 0; j < p.top; ++j) total += named[slot][j] == at[h] ? taken[slot][j] : 0.0f;
+            if (at[h] >= 0) spread[slot][at[h]] = total;
+        }
+        wave_meets();
+        if (own < p.rows) {
+            T* to = static_cast<T*>(p.dlogits) + own * p.dstride + first;
+            float v[R];
+            const float back = part * dot;
+#pragma unroll
+            for (int r = 0; r < R; ++r) v[r] = spread[slot][first + r] - (all ? e[r] * back : 0.0f);
+            constexpr int N = 16 / (int)sizeof(T);
+            if (R % N == 0 && first + R <= p.count) {
+#pragma unroll
+                for (int i = 0; i < R / N; ++i) store_quad(to + i * N, v + i * N);
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (first + r < p.count) to[r] = (T)v[r];
+            }
+        }
+        wave_meets();
+    }
+}
+
+template <typename T, int LANES, int R, int SCORE>
+hipError_t route_scores(const RouteParams& p, bool grad, hipStream_t s)
+{
+    constexpr int ROWS = kThreads / LANES;
+    const long long want = ((long long)p.rows + ROWS - 1) / ROWS;
+    const dim3 blocks((unsigned)(want < kRouteBlocks ? want : kRouteBlocks));
+    if (grad) hipLaunchKernelGGL((route_grad_kernel<T, LANES, R, SCORE>), blocks, dim3(kThreads), 0, s, p);
+    else if (sizeof(T) == 2 && !p.bias) hipLaunchKernelGGL((route_kernel<T, LANES, R, SCORE, sizeof(T) == 2>), blocks, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((route_kernel<T, LANES, R, SCORE, false>), blocks, dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+template <typename T, int LANES, int R>
+hipError_t route_rows(const RouteParams& p, bool grad, hipStream_t s)
+{
+    return p.score == kSoftmax ? route_scores<T, LANES, R, kSoftmax>(p, grad, s) : route_scores<T, LANES, R, kSigmoid>(p, grad, s);
+}
+// Lanes a row and experts a lane: 16 lanes where their registers hold the row, four rows a wave; groups have whole lanes of their own.
+template <typename T>
+hipError_t route_any(RouteParams p, bool grad, hipStream_t s)
+{
+    p.log_groups = 0;
+    while ((1 << p.log_groups) < p.groups) ++p.log_groups;
+    const int size = p.count / p.groups;
+    const auto part = [&](int lanes) { return lanes >> p.log_groups ? (size + (lanes >> p.log_groups) - 1) / (lanes >> p.log_groups) : 1 << 20; };
+    const int few = part(16), many = part(64);
+    if (few <= 1) return route_rows<T, 16, 1>(p, grad, s);
+    if (few <= 4) return route_rows<T, 16, 4>(p, grad, s);
+    if (few <= 8) return route_rows<T, 16, 8>(p, grad, s);
+    if (few <= 16) return route_rows<T, 16, 16>(p, grad, s);
+    if (many <= 8) return route_rows<T, 64, 8>(p, grad, s);
+    if (many <= 16) return route_rows<T, 64, 16>(p, grad, s);
+    return route_rows<T, 64, 32>(p, grad, s);
+}
+hipError_t route(const RouteParams& p, int dtype, bool grad, hipStream_t s)
+{
+    switch (dtype) {
+    case kF32: return route_any<float>(p, grad, s);
+    case kBf16: return route_any<__bf16>(p, grad, s);
+    default: return route_any<_Float16>(p, grad, s);
+    }
+}
+
+// ------------------------------------------------------------------ order
+// Counting sort, stable: an entry's place is the number of entries of smaller experts, and of its own in front of it.  Each workgroup has a run
+// of entries, each of its 16 waves a run of that; entries of no expert count as one expert more.
+constexpr int kOrderThreads = 1024, kOrderWaves = kOrderThreads / 64;
+
+__device__ __forceinline__ int expert_of(const OrderParams& p, int i)
+{
+    const int e = p.experts[i];
+    return (unsigned)e < (unsigned)p.count ? e : p.count;
+}
+
+// entries of each expert in a workgroup's run
+__global__ void __launch_bounds__(kOrderThreads) order_count_kernel(OrderParams p)
+{
+    __shared__ int counts[kMostRouted + 1];
+    for (int e = threadIdx.x; e <= p.count; e += kOrderThreads) counts[e] = 0;
+    __syncthreads();
+    const long long begin = (long long)blockIdx.x * p.share, end = begin + p.share < p.entries ? begin + p.share : p.entries;
+    for (long long i = begin + threadIdx.x; i < end; i += kOrderThreads) atomicAdd(&counts[expert_of(p, (int)i)], 1);
+    __syncthreads();
+    for (int e = threadIdx.x; e <= p.count; e += kOrderThreads) p.counts[(long long)blockIdx.x * (p.count + 1) + e] = counts[e];
+}
+
+__global__ void __launch_bounds__(kOrderThreads) order_kernel(OrderParams p)
+{
+    __shared__ int at[kOrderWaves][kMostRouted + 1];      // counts of a wave's run, then the places of its next entries
+    __shared__ int before[kMostRouted + 1], total[kMostRouted + 1];
+    __shared__ int ends_of_waves[kOrderWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bins = p.count + 1;
+    for (int e = threadIdx.x; e < kOrderWaves * bins; e += kOrderThreads) at[e / bins][e % bins] = 0;
+    for (int e = threadIdx.x; e < bins; e += kOrderThreads) before[e] = total[e] = 0;
+    __syncthreads();
+    const long long begin = (long long)blockIdx.x * p.share, end = begin + p.share < p.entries ? begin + p.share : p.entries;
+    const int run = (int)(((end - begin + kOrderWaves - 1) / kOrderWaves + 63) / 64 * 64);
+    const long long first = begin + (long long)wave * run, last = first + run < end ? first + run : end;
+    for (long long i = first + lane; i < last; i += 64) atomicAdd(&at[wave][expert_of(p, (int)i)], 1);
+    // what the workgroups in front have, and all of them
+    if (p.counts) {
+        // (several threads an expert where there are few)
+        const int parts = bins >= kOrderThreads ? 1 : kOrderThreads / bins;
+        for (int k = threadIdx.x; k < bins * parts; k += kOrderThreads) {
+            const int e = k % bins;
+            int all = 0, front = 0;
+            for (int b = k / bins; b < p.blocks; b += parts) {
+                const int c = p.counts[(long long)b * bins + e];
+                all += c;
+                front += b < (int)blockIdx.x ? c : 0;
+            }
+            if (all) atomicAdd(&total[e], all);
+            if (front) atomicAdd(&before[e], front);
+        }
+    }
+    __syncthreads();
+    if (!p.counts)
+        for (int e = threadIdx.x; e < bins; e += kOrderThreads) {
+            int all = 0;
+            for (int w = 0; w < kOrderWaves; ++w) all += at[w][e];
+            total[e] = all;
+        }
+    __syncthreads();
+    // sums over the experts in front: each thread one, up to 1025 (the last, of no expert, needs no place of its own in the scan)
+    const int e = threadIdx.x, own = e < p.count ? total[e] : 0;
+    int upto = own;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += other;
+    }
+    if (lane == 63) ends_of_waves[wave] = upto;
+    __syncthreads();
+    int in_front = 0;
+    for (int w = 0; w < wave; ++w) in_front += ends_of_waves[w];
+    upto += in_front;
+    if (blockIdx.x == 0 && e < p.count) p.ends[e] = upto;
+    int all = 0;
+    for (int w = 0; w < kOrderWaves; ++w) all += ends_of_waves[w];
+    if (e < p.count) {
+        int place = upto - own + before[e];
+        for (int w = 0; w < kOrderWaves; ++w) {
+            const int c = at[w][e];
+            at[w][e] = place;
+            place += c;
+        }
+    }
+    if (e == 0) {
+        int place = all + before[p.count];
+        for (int w = 0; w < kOrderWaves; ++w) {
+            const int c = at[w][p.count];
+            at[w][p.count] = place;
+            place += c;
+        }
+    }
+    __syncthreads();
+    // 64 entries at a time: those of the same expert find each other bit by bit
+    volatile int* mine = at[wave];
+    const int bits = 32 - __builtin_clz(p.count);
+    for (long long i0 = first; i0 < last; i0 += 64) {
+        const bool there = i0 + lane < last;
+        const int x = there ? expert_of(p, (int)(i0 + lane)) : p.count;
+        unsigned long long same = __ballot(there);
+        for (int b = 0; b < bits; ++b) {
+            const unsigned long long set = __ballot(x >> b & 1);
+            same &= x >> b & 1 ? set : ~set;
+        }
+        const int rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+        if (there) {
+            const int place = mine[x];
+            p.places[i0 + lane] = place + rank;
+            if (same >> lane == 1) mine[x] = place + rank + 1;      // the last of its kind
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_route(const RouteParams& p, int dtype, hipStream_t s) { return route(p, dtype, false, s); }
+hipError_t launch_route_grad(const RouteParams& p, int dtype, hipStream_t s) { return route(p, dtype, true, s); }
+
+void plan_order(OrderParams* p)
+{
+    // one workgroup for few entries (no second launch); otherwise up to 256 of at least 2048 entries each
+    if (p->entries <= 8192) {
+        p->blocks = 1;
+        p->share = p->entries;
+        return;
+    }
+    const int want = (p->entries + 2047) / 2048;
+    const int blocks = want < 256 ? want : 256;
+    p->share = (int)((((long long)p->entries + blocks - 1) / blocks + 63) / 64 * 64);
+    p->blocks = (int)(((long long)p->entries + p->share - 1) / p->share);
+}
+
+hipError_t launch_order(const OrderParams& p, hipStream_t s)
+{
+    if (p.blocks > 1) {
+        hipLaunchKernelGGL(order_count_kernel, dim3(p.blocks), dim3(kOrderThreads), 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(order_kernel, dim3(p.blocks), dim3(kOrderThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace spinner
