@@ -858,12 +858,13 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
         Quad quads[Lane::HALVES];
         float d[kPieceNumbers], v[kPieceNumbers];
         if (c < chunks) {
-            if constexpr (INT) fetch_chunk<Out>(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride, l.first, raw.k);
+            if constexpr (INT) fetch_chunk<Out, true>(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride, l.first, raw.k);
             else l.fetch(quads, static_cast<const Out*>(raw.x) + (at.lo + r) * raw.stride);
             if (raw.log > 0) l.diagonal(d, raw.diag, raw.norm);
         }
         if (k < runs) fetch(now, k);
         if (c < chunks) {
+            if constexpr (INT) settle_chunk<Out>(quads, in_row, l.first, raw.k);
             widen_quads<Out>(quads, v);
             if (raw.log > 0) Lane::within(v, d, raw.log, lane);
             if (raw.log > 9) Lane::meet(v, meeting + c * 128, lane);
@@ -875,7 +876,9 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
         }
         if constexpr (INT) {
             if (c < chunks) {
-                const int top = wave_largest(largest_bits(v, 0));
+                Largest most;
+                most.take(v);
+                const int top = wave_largest(most.bits());
                 if (lane == 0) largest[c] = top;
             }
             __syncthreads();
@@ -885,8 +888,9 @@ __global__ void __launch_bounds__(RAW ? 512 : 256, 2) few_rows_kernel(ProductPar
                 const RowScale s(top);
                 const float factor = flip ? -s.factor : s.factor;
                 unsigned code[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) code[i] = s.bad ? 0u : raw.log > 0 ? four_codes<false>(v + 4 * i, factor, 0.0f) : four_codes<true>(v + 4 * i, factor, s.scale);
+                if (raw.log > 0) eight_codes<false>(v, factor, s.scale, code);
+                else eight_codes<true>(v, factor, s.scale, code);
+                if (s.bad) code[0] = code[1] = 0;
                 unsigned* to = reinterpret_cast<unsigned*>(own_codes) + c * kCodePieces * 4;
                 if constexpr (Lane::HALVES == 1) *reinterpret_cast<uint2*>(to + lane * 2) = uint2{code[0], code[1]};
                 else { to[lane] = code[0]; to[64 + lane] = code[1]; }

@@ -156,42 +156,61 @@ struct Two {
 
 constexpr double kNever = -(double)INFINITY;
 constexpr int kCandidates = 48;                       // of a row, at most: its choices and what may lie level with the last of them
-constexpr float kNear = 4e-6f;                        // keys that lie nearer, in units of themselves and of the largest bias, may be the other way round
 
-// What decides, in fp64, from the row's logits in LDS: the groups that stay, and the choices, each the largest key behind the one before.  For rows
-// whose keys are too near each other in fp32; keys are made again for each choice, which few rows pay for and no register.
-template <int LANES, int R, int SCORE>
-__device__ __forceinline__ void choose64(const RouteParams& p, const float* logits, const Share& at, float top, int lane, double* group_keys, int* chosen)
-{
-    const float* l = logits + lane * R;
-    double sum = 0.0;
-    if constexpr (SCORE == kSoftmax) {
+// A row's scores in fp64, from its logits in LDS.
+template <int LANES, int SCORE>
+struct Scores64 {
+    const RouteParams& p;
+    double top = 0.0, sum = 1.0;
+    // `mine` logits of the lane at l
+    __device__ __forceinline__ Scores64(const RouteParams& p_, const float* l, int mine) : p(p_)
+    {
+        if constexpr (SCORE == kSoftmax) {
+            float high = -INFINITY;
 #pragma unroll 1
-        for (int r = 0; r < at.mine; ++r) sum += l[r] > -INFINITY ? exp((double)l[r] - (double)top) : 0.0;
-        sum = join_lanes<LANES>(sum, Sum{});
-    }
-    const auto score = [&](int r) {
-        const double s = SCORE == kSoftmax ? exp((double)l[r] - (double)top) / sum : 1.0 / (1.0 + exp(-(double)l[r]));
-        return l[r] > -INFINITY ? s + (p.bias ? (double)p.bias[at.first + r] : 0.0) : kNever;
-    };
-    bool stays = true;
-    if (p.groups > 1) {
-        const int each = LANES >> p.log_groups;
-        Two<double> two = {kNever, kNever};
+            for (int r = 0; r < mine; ++r) high = fmaxf(high, l[r]);
+            top = (double)join_lanes<LANES>(high, Larger{});
+            sum = 0.0;
 #pragma unroll 1
-        for (int r = 0; r < at.mine; ++r) two.take(p.bias || p.group_top > 1 ? score(r) : (double)l[r]);
-        two.lanes(each);
-        const double own = p.group_top > 1 && two.b > kNever ? two.a + two.b : two.a;
-        if ((lane & (each - 1)) == 0) group_keys[at.group] = own;
-        wave_meets();
-        int larger = 0;
-        for (int g = 0; g < p.groups; ++g) {
-            const double other = group_keys[g];
-            larger += (other > own) | ((other == own) & (g < at.group)) ? 1 : 0;
+            for (int r = 0; r < mine; ++r) sum += l[r] > -INFINITY ? exp((double)l[r] - top) : 0.0;
+            sum = join_lanes<LANES>(sum, Sum{});
         }
-        stays = larger < p.top_groups;
-        wave_meets();
     }
+    // score and bias of expert e
+    __device__ __forceinline__ double key(float l, int e) const
+    {
+        const double s = SCORE == kSoftmax ? exp((double)l - top) / sum : 1.0 / (1.0 + exp(-(double)l));
+        return l > -INFINITY ? s + (p.bias ? (double)p.bias[e] : 0.0) : kNever;
+    }
+};
+
+// whether this lane's group stays, in fp64
+template <int LANES, int SCORE>
+__device__ __forceinline__ bool stays64(const RouteParams& p, const float* l, const Share& at, int lane, double* group_keys)
+{
+    const Scores64<LANES, SCORE> scores(p, l, at.mine);
+    const int each = LANES >> p.log_groups;
+    Two<double> two = {kNever, kNever};
+#pragma unroll 1
+    for (int r = 0; r < at.mine; ++r) two.take(scores.key(l[r], at.first + r));
+    two.lanes(each);
+    const double own = p.group_top > 1 && two.b > kNever ? two.a + two.b : two.a;
+    if ((lane & (each - 1)) == 0) group_keys[at.group] = own;
+    wave_meets();
+    int larger = 0;
+    for (int g = 0; g < p.groups; ++g) {
+        const double other = group_keys[g];
+        larger += ((other > own) | ((other == own) & (g < at.group))) ? 1 : 0;
+    }
+    wave_meets();
+    return larger < p.top_groups;
+}
+
+// All choices in fp64, each the largest key behind the one before, for rows with more keys level with the last choice than there is room for.
+template <int LANES, int SCORE>
+__device__ __forceinline__ void choose64(const RouteParams& p, const float* l, const Share& at, bool stays, int lane, int* chosen)
+{
+    const Scores64<LANES, SCORE> scores(p, l, at.mine);
     double last = (double)INFINITY;
     int last_at = -1;
     for (int j = 0; j < p.top; ++j) {
@@ -199,10 +218,9 @@ __device__ __forceinline__ void choose64(const RouteParams& p, const float* logi
         int which = 0x7fffffff;
 #pragma unroll 1
         for (int r = 0; r < at.mine; ++r) {
-            const double k = p.bias ? score(r) : (double)l[r];
+            const double k = p.bias ? scores.key(l[r], at.first + r) : (double)l[r];
             const int own = at.first + r;
-            const bool behind = (k < last) | ((k == last) & (own > last_at));
-            const bool other = stays & behind & (k > v);
+            const bool other = stays & ((k < last) | ((k == last) & (own > last_at))) & (k > v);
             v = other ? k : v;
             which = other ? own : which;
         }
@@ -216,9 +234,8 @@ __device__ __forceinline__ void choose64(const RouteParams& p, const float* logi
 // LANES lanes a row, up to R neighbouring experts each, in registers from the logits to the choice.
 // A candidate is the largest of whole numbers of 32 bits below the last one: the first 22 of the key's bits in the order of the numbers, and 10 that put
 // equal ones in the order of their index.  EXACT (16-bit logits, no bias: the key is the logit, of which 22 bits are all there is): the candidates
-// are the choices.  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32;
-// rows with neighbours, or groups at the border, that fp32 does not tell apart (and that are not equal by having the same logit and bias) are
-// taken again by choose64.
+// are the choices.  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32; where those
+// lie too near each other (and are not equal by having the same logit and bias) by their keys in fp64, and so are groups at the border.
 template <typename T, int LANES, int R, int SCORE, bool EXACT>
 __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 {
@@ -250,7 +267,9 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
         }
         largest_bias = join_lanes<LANES>(largest_bias, Larger{});
     }
-    const auto reach = [&](float key) { return kNear * (__builtin_fabsf(key) + 2.0f * largest_bias); };
+    // Keys of fp32 that lie nearer may be the other way round.  A sigmoid is off by 4e-7 of itself, its key by 6e-8 more; a softmax by what its sum is off
+    // too, (R + 6) 2^-24, which two scores share.
+    const auto reach = [&](float key) { return (SCORE == kSigmoid ? 1.2e-6f : 5e-6f) * (__builtin_fabsf(key) + largest_bias); };
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
         const long long own = r0 + slot, row = own < p.rows ? own : p.rows - 1;
         float l[R];
@@ -310,6 +329,8 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
             // the border lies behind the last group that stays
             near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) & (mine - below <= reach(mine));
             wave_meets();
+            if (__builtin_expect(__ballot(near) != 0, 0)) stays = stays64<LANES, SCORE>(p, logits[slot] + lane * R, at, lane, group_keys[slot]);
+            near = false;
         }
         unsigned k[R];
 #pragma unroll
@@ -352,7 +373,6 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
                 if (j < p.top) chosen[slot][j] = order[slot][j] ? (int)(kLow - (order[slot][j] & kLow)) : -1;
             }
         } else {
-            near |= open;
             float v[HELD_ALL];
             int index[HELD_ALL], rank[HELD_ALL];
 #pragma unroll
@@ -375,11 +395,31 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 #pragma unroll
                 for (int h = 0; h < HELD_ALL; ++h) {
                     if (h * LANES >= count) break;
-                    const bool first = (other > v[h]) | ((other == v[h]) & (other_index < index[h]));
-                    rank[h] += first ? 1 : 0;
+                    rank[h] += ((other > v[h]) | ((other == v[h]) & (other_index < index[h]))) ? 1 : 0;
                     // logits without a bias are the keys; else equal logits with equal biases are equal
                     if (p.bias && (order[slot][i] != 0) & (v[h] > -INFINITY) & (other_index != index[h]) & (__builtin_fabsf(other - v[h]) <= reach(other)))
                         near |= (logits[slot][place(other_index)] != logits[slot][place(index[h])]) | (p.bias[other_index] != p.bias[index[h]]);
+                }
+            }
+            if (__builtin_expect(__ballot(near) != 0, 0)) {
+                const Scores64<LANES, SCORE> scores(p, logits[slot] + lane * R, at.mine);
+                double* keys = group_keys[slot];
+                static_assert(kCandidates <= kMostRouteGroups, "room for the candidates' keys");
+#pragma unroll 1
+                for (int j = lane; j < count; j += LANES) {
+                    const int own = (int)(kLow - (order[slot][j] & kLow));
+                    keys[j] = order[slot][j] ? scores.key(logits[slot][place(own)], own) : kNever;
+                }
+                wave_meets();
+#pragma unroll
+                for (int h = 0; h < HELD_ALL; ++h) {
+                    if (h * LANES >= count) break;
+                    const double mine = keys[h * LANES + lane < count ? h * LANES + lane : 0];
+                    rank[h] = 0;
+                    for (int i = 0; i < count; ++i) {
+                        const double other = keys[i];
+                        rank[h] += ((other > mine) | ((other == mine) & ((int)(kLow - (order[slot][i] & kLow)) < index[h]))) ? 1 : 0;
+                    }
                 }
             }
 #pragma unroll
@@ -389,19 +429,12 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 #pragma unroll
             for (int h = 0; h < HELD_ALL; ++h)
                 if (v[h] > -INFINITY && rank[h] < p.top) chosen[slot][rank[h]] = index[h];
-        }
-        near = any_lane<LANES>(near);
-        if (__builtin_expect(__ballot(near) != 0, 0)) {
-            __shared__ int again[ROWS][kMostChosen];
-            float highest = -INFINITY;
-            if constexpr (SCORE == kSoftmax) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) highest = fmaxf(highest, l[r]);
-                highest = join_lanes<LANES>(highest, Larger{});
+            open = any_lane<LANES>(open);
+            if (__builtin_expect(__ballot(open) != 0, 0)) {
+                // (a row that is not open gets what it has)
+                wave_meets();
+                choose64<LANES, SCORE>(p, logits[slot] + lane * R, at, stays, lane, chosen[slot]);
             }
-            choose64<LANES, R, SCORE>(p, logits[slot], at, highest, lane, group_keys[slot], again[slot]);
-            if (near)
-                for (int j = lane; j < p.top; j += LANES) chosen[slot][j] = again[slot][j];
         }
         wave_meets();
         // weights: choice j is lane j mod LANES's
