@@ -61,14 +61,16 @@ template <int MASK> __device__ __forceinline__ void pair_across(double v, double
 }
 
 // ------------------------------------------------------------------ lanes of a row
-// `op` over a row's LANES lanes (16: a row of the instruction set's own, joined in its registers), in all of them
+// `op` over a row's LANES lanes (4, 16: joined in registers by the instruction set's own quads and rows), in all of them
 template <int LANES, typename V, typename F>
 __device__ __forceinline__ V join_lanes(V v, F op)
 {
     v = op(v, across<1>(v));
     v = op(v, across<2>(v));
-    v = op(v, across<4>(v));
-    v = op(v, across<8>(v));
+    if constexpr (LANES > 4) {
+        v = op(v, across<4>(v));
+        v = op(v, across<8>(v));
+    }
     if constexpr (LANES == 64) {
         V a, b;
         pair_across<16>(v, a, b);
@@ -85,7 +87,7 @@ __device__ __forceinline__ bool any_lane(bool v)
 {
     const unsigned long long all = __ballot(v);
     if constexpr (LANES == 64) return all != 0;
-    return (all >> (threadIdx.x & 48) & 0xffff) != 0;
+    return (all >> (threadIdx.x & (64 - LANES)) & ((1ull << LANES) - 1)) != 0;
 }
 
 // What the wave's lanes have written to LDS, in order, is there for all of them: the LDS keeps the order of a wave, and so has the compiler to.
@@ -171,9 +173,14 @@ struct Two {
     V a, b;
     __device__ __forceinline__ void take(V k)
     {
-        const V low = a < k ? a : k;
-        b = b > low ? b : low;
-        a = a > k ? a : k;
+        if constexpr (sizeof(V) == 4) {
+            b = __builtin_amdgcn_fmed3f(a, b, k);
+            a = fmaxf(a, k);
+        } else {
+            const V low = a < k ? a : k;
+            b = b > low ? b : low;
+            a = a > k ? a : k;
+        }
     }
     __device__ __forceinline__ void merge(V a2, V b2)
     {
@@ -203,7 +210,9 @@ struct Two {
 };
 
 constexpr double kNever = -(double)INFINITY;
-constexpr int kCandidates = 48;                       // of a row, at most: its choices and what may lie level with the last of them
+// most choices of a row of so many lanes, and candidates: its choices and what may lie level with the last of them
+constexpr int most_chosen(int lanes) { return lanes == 4 ? 8 : kMostChosen; }
+constexpr int most_candidates(int lanes) { return lanes == 4 ? 16 : 48; }
 
 // A row's scores in fp64, from its logits in LDS.
 template <int LANES, int SCORE>
@@ -285,15 +294,16 @@ __device__ __forceinline__ void choose64(const RouteParams& p, const float* l, c
 // are the choices.  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32; where those
 // lie too near each other (and are not equal by having the same logit and bias) by their keys in fp64, and so are groups at the border.
 template <typename T, int LANES, int R, int SCORE, bool EXACT>
-__global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
+__global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteParams p)
 {
-    constexpr int ROWS = kThreads / LANES, HELD = (kMostChosen + LANES - 1) / LANES, HELD_ALL = (kCandidates + LANES - 1) / LANES;
-    constexpr unsigned kLow = LANES * R > 1024 ? 2047 : 1023;
+    constexpr int ROWS = kThreads / LANES, MOST = most_chosen(LANES), CANDIDATES = most_candidates(LANES);
+    constexpr int HELD = (MOST + LANES - 1) / LANES, HELD_ALL = (CANDIDATES + LANES - 1) / LANES;
+    constexpr unsigned kLow = LANES * R > 1024 ? 2047 : 1023, kLeast = 0x00800000u;      // kLeast: of the numbers above -inf
     __shared__ float logits[ROWS][LANES * R];
-    __shared__ double group_keys[ROWS][kMostRouteGroups];
-    __shared__ unsigned order[ROWS][kCandidates];
-    __shared__ float keys_of[EXACT ? 1 : ROWS][EXACT ? 1 : kCandidates + 1];
-    __shared__ int chosen[ROWS][kMostChosen];
+    __shared__ double group_keys[ROWS][LANES > CANDIDATES ? LANES : CANDIDATES + 1];     // (no more groups than lanes)
+    __shared__ unsigned order[ROWS][CANDIDATES];
+    __shared__ float keys_of[EXACT ? 1 : ROWS][EXACT ? 1 : CANDIDATES + 1];
+    __shared__ int chosen[ROWS][MOST];
     const int lane = threadIdx.x & (LANES - 1), slot = threadIdx.x / LANES, size = p.count / p.groups;
     const Share at(lane, LANES, p.log_groups, p.groups, size);
     const int each = LANES >> p.log_groups, part_of = (size + each - 1) / each;
@@ -303,6 +313,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
         return l / each * size + (l & (each - 1)) * part_of + (place & (R - 1));
     };
     float bias[R], largest_bias = 0.0f;
+    bool bad_bias = false;
 #pragma unroll
     for (int r = 0; r < R; ++r) bias[r] = 0.0f;
     if (!EXACT && p.bias) {
@@ -310,6 +321,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             bias[r] = r < at.mine ? bias[r] : 0.0f;
+            bad_bias |= bias[r] != bias[r];
             // (infinities are far from all others)
             largest_bias = fmaxf(largest_bias, __builtin_fabsf(bias[r]) < INFINITY ? __builtin_fabsf(bias[r]) : 0.0f);
         }
@@ -323,13 +335,21 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
         float l[R];
         load_logits<T, R>(l, static_cast<const T*>(p.logits) + row * p.stride, at.first, at.mine, p.count);
         const bool routed = !p.mask || p.mask[row] != 0;
-        bool bad = false;                  // a NaN, or an infinity in a softmax
+        // what is no number, no expert, or far from the ordinary is looked at where there is any
+        bool odd = bad_bias;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            bad |= (l[r] != l[r]) | (bias[r] != bias[r]) | (SCORE == kSoftmax && l[r] == INFINITY);
+            odd |= !(__builtin_fabsf(l[r]) <= 32.0f);
             logits[slot][lane * R + r] = l[r];
         }
-        bad = any_lane<LANES>(bad);
+        const bool careful = __ballot(odd) != 0;
+        bool bad = false;                  // a NaN, or an infinity in a softmax
+        if (careful) {
+            bad = bad_bias;
+#pragma unroll
+            for (int r = 0; r < R; ++r) bad |= (l[r] != l[r]) | (SCORE == kSoftmax && l[r] == INFINITY);
+            bad = any_lane<LANES>(bad);
+        }
         float top = -INFINITY, sum = 0.0f;
         const bool scored = (!EXACT && p.bias) || p.group_top > 1;
         float key[R];
@@ -337,23 +357,36 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 #pragma unroll
             for (int r = 0; r < R; ++r) top = fmaxf(top, l[r]);
             top = join_lanes<LANES>(top, Larger{});
+            if (p.renormalise) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                key[r] = exp_below(l[r] - top);
-                sum += key[r];
+                for (int r = 0; r < R; ++r) {
+                    key[r] = __builtin_amdgcn_exp2f(fmaxf(l[r] - top, -200.0f) * 1.44269502f);
+                    sum += key[r];
+                }
+            } else {                       // the weights are these over this sum
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    key[r] = exp_below(l[r] - top);
+                    sum += key[r];
+                }
             }
             sum = join_lanes<LANES>(sum, Sum{});
         }
-        // keys, -inf for what cannot be chosen
+        // Keys, -inf for what cannot be chosen.  Scores of all experts in few instructions, off by 64 (x up to -88: 88) times 6e-8 of themselves at most and
+        // 4e-7; the candidates' are made again.
         const float part = 1.0f / sum;
+        if (scored) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (scored) {
-                const float s = SCORE == kSoftmax ? key[r] * part : sigmoid(l[r]);
-                key[r] = l[r] > -INFINITY ? s + bias[r] : -INFINITY;
-            } else {
-                key[r] = l[r];
+            for (int r = 0; r < R; ++r) {
+                const float s = SCORE == kSoftmax ? key[r] * part : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(l[r] * -1.44269502f));
+                key[r] = s + bias[r];
             }
+            if (careful)
+#pragma unroll
+                for (int r = 0; r < R; ++r) key[r] = l[r] > -INFINITY ? key[r] : -INFINITY;
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) key[r] = l[r];
         }
         bool near = false, stays = true;
         if (p.groups > 1) {
@@ -376,7 +409,8 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
             }
             stays = larger < p.top_groups;
             // the border lies behind the last group that stays
-            near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) & (mine - below <= reach(mine));
+            near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) &
+                   (mine - below <= ((careful || SCORE == kSoftmax) ? 1.2e-5f : 5e-6f) * (__builtin_fabsf(mine) + largest_bias));
             wave_meets();
             if (__builtin_expect(__ballot(near) != 0, 0)) stays = stays64<LANES, SCORE>(p, logits[slot] + lane * R, at, lane, group_keys[slot]);
             near = false;
@@ -385,7 +419,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const float v = EXACT || !p.bias ? l[r] : key[r];
-            k[r] = stays && v > -INFINITY ? (ordered(v) & ~kLow) | (kLow - (unsigned)(lane * R + r)) : 0;
+            k[r] = (ordered(v) & ~kLow) | (kLow - (unsigned)(lane * R + r));
         }
         // the largest number below the last one, which leaves it the largest of the differences to that, modulo 2^32
         unsigned last = 0xffffffffu;
@@ -399,8 +433,8 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
                 const unsigned t = k[r] - last;
                 best = t > best ? t : best;
             }
-            const unsigned next = join_lanes<LANES>(best, Larger{}) + last;
-            last = next < last ? next : 0;
+            const unsigned next = join_lanes<LANES>(stays ? best : 0u, Larger{}) + last;
+            last = ((next < last) & (next >= kLeast)) ? next : 0;
             if (lane == 0) order[slot][count] = last;
             ++count;
             if constexpr (EXACT) {
@@ -411,7 +445,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
                 if (count == p.top) border = v;
                 else open = open & (last != 0) & (border - v <= reach(border) + 5e-4f * __builtin_fabsf(border) + 1e-40f);
                 if (count > p.top && __ballot(open) == 0) break;
-                if (count == kCandidates) break;
+                if (count == CANDIDATES) break;
             }
         }
         wave_meets();
@@ -430,6 +464,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
                 v[h] = -INFINITY;
                 own_place[h] = 0x7fffffff;
                 rank[h] = 0;
+                if (h * LANES >= count) continue;
                 if (j < count && order[slot][j]) {
                     own_place[h] = (int)(kLow - (order[slot][j] & kLow));
                     const float x = logits[slot][own_place[h]];
@@ -444,13 +479,12 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
                 const int other_place = (int)(kLow - (order[slot][i] & kLow));
 #pragma unroll
                 for (int h = 0; h < HELD_ALL; ++h)
-                    if (h == 0 || h * LANES < count) rank[h] += ((other > v[h]) | ((other == v[h]) & (other_place < own_place[h]))) ? 1 : 0;
+                    if (h * LANES < count) rank[h] += ((other > v[h]) | ((other == v[h]) & (other_place < own_place[h]))) ? 1 : 0;
             }
             wave_meets();
             if (p.bias) {
                 // keys next to each other in this order that may be the other way round, unless they are of equal logits and biases
                 int* places = reinterpret_cast<int*>(group_keys[slot]);
-                static_assert(sizeof(double) * kMostRouteGroups >= sizeof(int) * (kCandidates + 1), "room for the candidates");
 #pragma unroll
                 for (int h = 0; h < HELD_ALL; ++h)
                     if (v[h] > -INFINITY) { keys_of[slot][rank[h] + 1] = v[h]; places[rank[h] + 1] = own_place[h]; }
@@ -469,7 +503,6 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
             if (__builtin_expect(__ballot(near) != 0, 0)) {
                 const Scores64<LANES, SCORE> scores(p, logits[slot] + lane * R, at.mine);
                 double* keys = group_keys[slot];
-                static_assert(kCandidates <= kMostRouteGroups, "room for the candidates' keys");
 #pragma unroll 1
                 for (int j = lane; j < count; j += LANES) {
                     const int own = (int)(kLow - (order[slot][j] & kLow));
@@ -549,18 +582,22 @@ __global__ void __launch_bounds__(kThreads) route_kernel(RouteParams p)
 template <typename T, int LANES, int R, int SCORE>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
 {
-    constexpr int ROWS = kThreads / LANES, HELD = (kMostChosen + LANES - 1) / LANES;
+    constexpr int ROWS = kThreads / LANES, MOST = most_chosen(LANES), HELD = (MOST + LANES - 1) / LANES;
     __shared__ float spread[ROWS][LANES * R];
-    __shared__ float taken[ROWS][kMostChosen];
-    __shared__ int named[ROWS][kMostChosen];
-    const int lane = threadIdx.x & (LANES - 1), first = lane * R, slot = threadIdx.x / LANES;
+    __shared__ float taken[ROWS][MOST];
+    __shared__ int named[ROWS][MOST];
+    // a lane has pieces of 16 bytes, the lanes' side by side (neighbours alone would meet in few banks of LDS: 8191 x 999 in fp32 18.1 us)
+    constexpr int N = 16 / (int)sizeof(T), PIECE = R % N == 0 ? N : 1, PIECES = R / PIECE;
+    const int lane = threadIdx.x & (LANES - 1), slot = threadIdx.x / LANES;
+    const auto first = [&](int i) { return (i * LANES + lane) * PIECE; };
     const bool all = SCORE == kSoftmax && !p.renormalise;          // every logit has a gradient, not the chosen ones alone
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
         const long long own = r0 + slot, row = own < p.rows ? own : p.rows - 1;
         const T* from = static_cast<const T*>(p.logits) + row * p.stride;
         float e[R], top = -INFINITY, sum = 0.0f;
         if (all) {
-            load_logits<T, R>(e, from, first, p.count - first, p.count);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) load_logits<T, PIECE>(reinterpret_cast<float(&)[PIECE]>(e[i * PIECE]), from, first(i), p.count - first(i), p.count);
 #pragma unroll
             for (int r = 0; r < R; ++r) top = fmaxf(top, e[r]);
             top = join_lanes<LANES>(top, Larger{});
@@ -610,7 +647,9 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
             if (j < p.top) { taken[slot][j] = at[h] >= 0 ? d[h] : 0.0f; named[slot][j] = at[h]; }
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) spread[slot][first + r] = 0.0f;
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int k = 0; k < PIECE; ++k) spread[slot][first(i) + k] = 0.0f;
         wave_meets();
         // an expert that a row names more than once: the sum, in the order of the choices, written by each of them
 #pragma unroll
@@ -621,19 +660,20 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
         }
         wave_meets();
         if (own < p.rows) {
-            T* to = static_cast<T*>(p.dlogits) + own * p.dstride + first;
-            float v[R];
+            T* to = static_cast<T*>(p.dlogits) + own * p.dstride;
             const float back = part * dot;
 #pragma unroll
-            for (int r = 0; r < R; ++r) v[r] = spread[slot][first + r] - (all ? e[r] * back : 0.0f);
-            constexpr int N = 16 / (int)sizeof(T);
-            if (R % N == 0 && first + R <= p.count) {
+            for (int i = 0; i < PIECES; ++i) {
+                float v[PIECE];
 #pragma unroll
-                for (int i = 0; i < R / N; ++i) store_quad(to + i * N, v + i * N);
-            } else {
+                for (int k = 0; k < PIECE; ++k) v[k] = spread[slot][first(i) + k] - (all ? e[i * PIECE + k] * back : 0.0f);
+                if (PIECE == N && first(i) + N <= p.count) {
+                    store_quad(to + first(i), v);
+                } else {
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-                    if (first + r < p.count) to[r] = (T)v[r];
+                    for (int k = 0; k < PIECE; ++k)
+                        if (first(i) + k < p.count) to[first(i) + k] = (T)v[k];
+                }
             }
         }
         wave_meets();
@@ -656,8 +696,8 @@ hipError_t route_rows(const RouteParams& p, bool grad, hipStream_t s)
 {
     return p.score == kSoftmax ? route_scores<T, LANES, R, kSoftmax>(p, grad, s) : route_scores<T, LANES, R, kSigmoid>(p, grad, s);
 }
-// Lanes a row and experts a lane: 16 lanes where their registers hold the row, four rows a wave, but 64 for so few rows that waves are to spare; groups have
-// whole lanes of their own.
+// Lanes a row and experts a lane: four lanes where their registers hold the row, 16 rows a wave, then 16, but 64 for so few rows that waves are to spare;
+// groups have whole lanes of their own.
 template <typename T>
 hipError_t route_any(RouteParams p, bool grad, hipStream_t s)
 {
@@ -665,10 +705,14 @@ hipError_t route_any(RouteParams p, bool grad, hipStream_t s)
     while ((1 << p.log_groups) < p.groups) ++p.log_groups;
     const int size = p.count / p.groups;
     const auto part = [&](int lanes) { return lanes >> p.log_groups ? (size + (lanes >> p.log_groups) - 1) / (lanes >> p.log_groups) : 1 << 20; };
-    const int few = part(16), many = part(64);
+    const int least = p.top <= most_chosen(4) ? part(4) : 1 << 20, few = part(16), many = part(64);
     if (p.rows <= kFewRouteRows && !grad) {
         if (many <= 1) return route_rows<T, 64, 1>(p, grad, s);
         if (many <= 4) return route_rows<T, 64, 4>(p, grad, s);
+    }
+    if (p.rows > kFewRouteRows) {
+        if (least <= 8) return route_rows<T, 4, 8>(p, grad, s);
+        if (least <= 16) return route_rows<T, 4, 16>(p, grad, s);
     }
     if (few <= 1) return route_rows<T, 16, 1>(p, grad, s);
     if (few <= 4) return route_rows<T, 16, 4>(p, grad, s);
