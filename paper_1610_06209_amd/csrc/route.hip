@@ -734,12 +734,24 @@ hipError_t route(const RouteParams& p, int dtype, bool grad, hipStream_t s)
 // ------------------------------------------------------------------ order
 // Counting sort, stable: an entry's place is the number of entries of smaller experts, and of its own in front of it.  Each workgroup has a run
 // of entries, each of its 16 waves a run of that; entries of no expert count as one expert more.
-constexpr int kOrderThreads = 1024;
+constexpr int kOrderThreads = 1024, kHeld = 4;
+// Threads of the kernel that orders and the most experts that it has room for in LDS.
+constexpr int kFewExperts = 256;
+constexpr int order_threads(int count) { return count <= kFewExperts ? 1024 : 512; }
 
 __device__ __forceinline__ int expert_of(const OrderParams& p, int i)
 {
     const int e = p.experts[i];
     return (unsigned)e < (unsigned)p.count ? e : p.count;
+}
+
+// One more entry of expert x, for the lanes that have one.  Entries of no expert come in long runs (padding), and are counted at once: so many lanes
+// at one place of LDS would wait for each other.
+__device__ __forceinline__ void count_entry(int* counts, int x, bool there, int none)
+{
+    const unsigned long long of_none = __ballot(there && x == none);
+    if (there && x != none) atomicAdd(&counts[x], 1);
+    if (of_none && (threadIdx.x & 63) == (unsigned)__builtin_ctzll(of_none)) atomicAdd(&counts[none], __builtin_popcountll(of_none));
 }
 
 // entries of each expert in a workgroup's run
@@ -749,60 +761,83 @@ __global__ void __launch_bounds__(kOrderThreads) order_count_kernel(OrderParams 
     for (int e = threadIdx.x; e <= p.count; e += kOrderThreads) counts[e] = 0;
     __syncthreads();
     const long long begin = (long long)blockIdx.x * p.share, end = begin + p.share < p.entries ? begin + p.share : p.entries;
-    for (long long i = begin + threadIdx.x; i < end; i += kOrderThreads) atomicAdd(&counts[expert_of(p, (int)i)], 1);
+    for (long long i0 = begin; i0 < end; i0 += kOrderThreads) {
+        const long long i = i0 + threadIdx.x;
+        count_entry(counts, i < end ? expert_of(p, (int)i) : p.count, i < end, p.count);
+    }
     __syncthreads();
     for (int e = threadIdx.x; e <= p.count; e += kOrderThreads) p.counts[(long long)blockIdx.x * (p.count + 1) + e] = counts[e];
 }
 
-template <int THREADS>
+template <int THREADS, int MOST>
 __global__ void __launch_bounds__(THREADS) order_kernel(OrderParams p)
 {
-    constexpr int WAVES = THREADS / 64, EACH = kMostRouted / THREADS;
-    __shared__ int at[WAVES][kMostRouted + 1];            // counts of a wave's run, then the places of its next entries
-    __shared__ int before[kMostRouted + 1], total[kMostRouted + 1];
+    constexpr int WAVES = THREADS / 64, EACH = (MOST + THREADS - 1) / THREADS;
+    __shared__ int at[WAVES][MOST + 1];                   // counts of a wave's run, then the places of its next entries
+    __shared__ unsigned long long alike[WAVES][MOST + 1]; // lanes with an entry of this expert
+    __shared__ int before[MOST + 1], total[MOST + 1];
     __shared__ int ends_of_waves[WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bins = p.count + 1;
     const long long begin = (long long)blockIdx.x * p.share, end = begin + p.share < p.entries ? begin + p.share : p.entries;
     const int run = (int)(((end - begin + WAVES - 1) / WAVES + 63) / 64 * 64);
     const long long first = begin + (long long)wave * run, last = first + run < end ? first + run : end;
-    for (int e = lane; e < bins; e += 64) at[wave][e] = 0;
-    for (int e = threadIdx.x; e < bins; e += THREADS) before[e] = total[e] = 0;
-    __syncthreads();
-    for (long long i = first + lane; i < last; i += 64) atomicAdd(&at[wave][expert_of(p, (int)i)], 1);
+    // the first kHeld entries of a lane stay in registers for both looks at them
+    int held[kHeld];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+        const long long i = first + u * 64 + lane;
+        held[u] = i < last ? p.experts[i] : -1;
+    }
+    for (int e = lane; e < bins; e += 64) {
+        at[wave][e] = 0;
+        alike[wave][e] = 0;
+    }
     // what the workgroups in front have, and all of them
     if (p.counts) {
-        // (several threads an expert where there are few; eight counts on their way at a time: one by one, 131064 entries of 256 experts 11.2 us)
+        // (several threads an expert where there are few; sixteen counts on their way at a time)
+        for (int e = threadIdx.x; e < bins; e += THREADS) before[e] = total[e] = 0;
+        __syncthreads();
         const int parts = bins >= THREADS ? 1 : THREADS / bins;
         for (int k = threadIdx.x; k < bins * parts; k += THREADS) {
             const int e = k % bins;
             int all = 0, front = 0;
-            for (int b0 = k / bins; b0 < p.blocks; b0 += 8 * parts) {
-                int c[8];
+            for (int b0 = k / bins; b0 < p.blocks; b0 += 16 * parts) {
+                int c[16];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
+                for (int u = 0; u < 16; ++u) {
                     const int b = b0 + u * parts;
-                    c[u] = p.counts[(long long)(b < p.blocks ? b : b0) * bins + e];
+                    c[u] = b < p.blocks ? p.counts[(long long)b * bins + e] : 0;
                 }
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int b = b0 + u * parts;
-                    all += b < p.blocks ? c[u] : 0;
-                    front += b < (int)blockIdx.x ? c[u] : 0;
+                for (int u = 0; u < 16; ++u) {
+                    all += c[u];
+                    front += b0 + u * parts < (int)blockIdx.x ? c[u] : 0;
                 }
             }
             if (all) atomicAdd(&total[e], all);
             if (front) atomicAdd(&before[e], front);
         }
-    } else {
-        __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+        held[u] = (unsigned)held[u] < (unsigned)p.count ? held[u] : p.count;
+        count_entry(at[wave], held[u], first + u * 64 + lane < last, p.count);
+    }
+    for (long long i0 = first + kHeld * 64; i0 < last; i0 += 64) {
+        const bool there = i0 + lane < last;
+        count_entry(at[wave], there ? expert_of(p, (int)(i0 + lane)) : p.count, there, p.count);
+    }
+    __syncthreads();
+    if (!p.counts) {
         for (int e = threadIdx.x; e < bins; e += THREADS) {
             int all = 0;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) all += at[w][e];
             total[e] = all;
+            before[e] = 0;
         }
+        __syncthreads();
     }
-    __syncthreads();
     // sums over the experts in front, EACH neighbours a thread (the last, of no expert, has its place behind all of them)
     int own[EACH], upto = 0;
 #pragma unroll
@@ -845,23 +880,31 @@ __global__ void __launch_bounds__(THREADS) order_kernel(OrderParams p)
     }
     if (threadIdx.x == 0) places_from(p.count, all + before[p.count]);
     __syncthreads();
-    // 64 entries at a time: those of the same expert find each other bit by bit
+    // 64 entries at a time: each lane leaves its bit with its expert, and finds there who else did (comparing the experts' numbers bit by bit: 8192 entries
+    // of one workgroup 10.6 us)
     volatile int* next = at[wave];
-    const int bits = 32 - __builtin_clz(p.count);
-    for (long long i0 = first; i0 < last; i0 += 64) {
-        const bool there = i0 + lane < last;
-        const int x = there ? expert_of(p, (int)(i0 + lane)) : p.count;
-        unsigned long long same = __ballot(there);
-        for (int b = 0; b < bits; ++b) {
-            const unsigned long long set = __ballot(x >> b & 1);
-            same &= x >> b & 1 ? set : ~set;
-        }
-        const int rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+    volatile unsigned long long* mine_of = alike[wave];
+    const auto place = [&](long long i, int x, bool there) {
+        const unsigned long long of_none = __ballot(there && x == p.count);
+        if (there && x != p.count) atomicOr(&alike[wave][x], 1ull << lane);
+        wave_meets();
         if (there) {
-            const int place = next[x];
-            p.places[i0 + lane] = place + rank;
-            if (same >> lane == 1) next[x] = place + rank + 1;      // the last of its kind
+            const unsigned long long same = x == p.count ? of_none : mine_of[x];
+            const int at = next[x], rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+            p.places[i] = at + rank;
+            if (same >> lane == 1) {                             // the last of its kind
+                next[x] = at + rank + 1;
+                mine_of[x] = 0;
+            }
         }
+        wave_meets();
+    };
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+        if (first + u * 64 < last) place(first + u * 64 + lane, held[u], first + u * 64 + lane < last);
+    for (long long i0 = first + kHeld * 64; i0 < last; i0 += 64) {
+        const bool there = i0 + lane < last;
+        place(i0 + lane, there ? expert_of(p, (int)(i0 + lane)) : p.count, there);
     }
 }
 
@@ -872,13 +915,13 @@ hipError_t launch_route_grad(const RouteParams& p, int dtype, hipStream_t s) { r
 
 void plan_order(OrderParams* p)
 {
-    // one workgroup for few entries (no second launch); otherwise up to 256 of at least 2048 entries each
+    // one workgroup for few entries (no second launch); otherwise up to 256 of at least as many entries as lie in registers
     if (p->entries <= 8192) {
         p->blocks = 1;
         p->share = p->entries;
         return;
     }
-    const int want = (p->entries + 2047) / 2048;
+    const int least = order_threads(p->count) * kHeld, want = (p->entries + least - 1) / least;
     const int blocks = want < 256 ? want : 256;
     p->share = (int)((((long long)p->entries + blocks - 1) / blocks + 63) / 64 * 64);
     p->blocks = (int)(((long long)p->entries + p->share - 1) / p->share);
@@ -891,8 +934,9 @@ hipError_t launch_order(const OrderParams& p, hipStream_t s)
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (p.entries <= kFewEntries) hipLaunchKernelGGL(order_kernel<256>, dim3(1), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(order_kernel<kOrderThreads>, dim3(p.blocks), dim3(kOrderThreads), 0, s, p);
+    if (p.entries <= kFewEntries) hipLaunchKernelGGL((order_kernel<256, kMostRouted>), dim3(1), dim3(256), 0, s, p);
+    else if (p.count <= kFewExperts) hipLaunchKernelGGL((order_kernel<order_threads(kFewExperts), kFewExperts>), dim3(p.blocks), dim3(order_threads(kFewExperts)), 0, s, p);
+    else hipLaunchKernelGGL((order_kernel<order_threads(kMostRouted), kMostRouted>), dim3(p.blocks), dim3(order_threads(kMostRouted)), 0, s, p);
     return hipGetLastError();
 }
 
