@@ -427,10 +427,12 @@ product_kernel(ProductParams p)
         RowTiles<BM> tiles(p);
         unsigned tile;
         if (!xcd_run(p.first_block + blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
-        // bands of four row tiles, column by column
-        const unsigned band = tile / (4 * columns), in_band = tile - band * 4 * columns;
-        const unsigned height = (unsigned)tiles.total - 4 * band < 4 ? tiles.total - 4 * band : 4;
-        const RowTile at = tiles.find(4 * band + in_band % height);
+        // bands of four row tiles, column by column (8 bits: eight, of which more are of one expert; 16382 uneven rows of 16 experts, 4096 to 4096, bands of
+        // 2 / 4 / 8 / 16 342 / 354 / 336 / 342 us, one weight matrix of 8192 to 8192 967 / 945 / 946 / 972)
+        constexpr unsigned BAND = INT ? 8 : 4;
+        const unsigned band = tile / (BAND * columns), in_band = tile - band * BAND * columns;
+        const unsigned height = (unsigned)tiles.total - BAND * band < BAND ? tiles.total - BAND * band : BAND;
+        const RowTile at = tiles.find(BAND * band + in_band % height);
         const int n0 = in_band / height * BN;
         const bool nobody = at.expert == p.experts;
         a = p.a + at.lo * p.a_stride;
