@@ -525,7 +525,8 @@ size_t spinner_grouped_matmul_dw_workspace_bytes(long rows, int n, int k, int ex
  *   places    in   device int32 [rows][top] or NULL (top = 1).  The codes and the
  *                  scale of row r go to each of the places in its row of `places`
  *                  (see spinner_route_order) of [rows * top]; NULL: to place r.
- *                  Places outside [0, rows * top) are passed over.
+ *                  Places outside [0, rows * top) are passed over; what several
+ *                  rows name is undefined.
  *   top       in   1 <= top <= 32, rows * top <= 2^31 - 2^16
  *   codes     out  device int8 [rows * top][width]
  *   scales    out  device fp32 [rows * top]
@@ -636,7 +637,7 @@ int spinner_route_order(const int *chosen, long count, int experts, int *places,
  * weights and dweights fp32 [rows][top].  Sums are fp32 and j (i) in a fixed order.
  * Places outside [0, rows * top) are passed over (their dweights are 0); a row of
  * dispatch's out or of dy that no place names is left as it was, one that several
- * name is one of theirs.  In spinner_combine what has the weight 0 adds nothing,
+ * name holds parts of any of theirs.  In spinner_combine what has the weight 0 adds nothing,
  * whatever its row holds.  1 <= n <= 2^24, 1 <= top <= 32, rows * top <= 2^31 - 2^16,
  * strides >= 0 (results: >= n) elements.
  */

@@ -78,7 +78,7 @@ int fused_max_log(int epilogue)
 
 extern "C" {
 
-int spinner_version(void) { return 140; }
+int spinner_version(void) { return 150; }
 
 const char* spinner_strerror(int status)
 {
