@@ -15,7 +15,8 @@ __device__ __forceinline__ void waves_meet()
 
 // Rows to codes and scales, v = H D x on each run of 2^log coordinates first.  A row is WAVES waves' (1: four rows a workgroup; 8: one), HOLD chunks of
 // 512 numbers each, which stay in registers from the largest magnitude to the codes; SWEEP: longer rows, which are read, and rotated, twice.
-// Each of a row's slots gets the codes.
+// Each of a row's slots gets the codes.  16384 x 8192 without a rotation fp32 110 us, bf16 68, 6.1 and 5.9 TB/s, as fast as a copy; rotated in runs of 32 67, of 512 101, of 4096 124, where
+// the butterflies' vector instructions bound it.
 template <typename T, int LOG, int WAVES, int HOLD, bool SWEEP>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) int_quantize_kernel(IntQuantizeParams p)
 {
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) int_quantize_ke
     }
 }
 
-// Codes back to numbers, eight a lane, LANES lanes a row.
+// Codes back to numbers, eight a lane, LANES lanes a row.  16384 x 8192 to bf16, 403 MB, 66 us, 6.1 TB/s: as fast as a copy.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) int_dequantize_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales, int rows, int k, int width,
                                                              T* __restrict__ out, long long out_stride)

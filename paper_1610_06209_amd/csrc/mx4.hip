@@ -210,7 +210,8 @@ void plan_product(int direction, bool mx4, ProductParams* p)
     else shortest(kForms16, direction, 64, p);
 }
 
-// (a chunk of 128 whole numbers takes the loads, reads and products of one of 64 numbers of 16 bits)
+// (A chunk of 128 whole numbers takes the loads, reads and products of one of 64 numbers of 16 bits.)  8 bits, k = n = 4096, us for 100 / 300 / 1000 / 2000 / 16384 (8 experts) rows: 256 x 256 44 / 45 / 47 / 48 /
+// 253, 128 x 128 25 / 25 / 27 / 39 / 331, with four chunks in LDS 19 / 20 / 24 / 43 / 361, 64 x 64 11 / 16 / 32 / 60 / 507; n = 16384 with 16 / 17 rows 64 x 64 18.5 / 18.5, few rows 18.5 / 25.7
 void plan_product_int(ProductParams* p)
 {
     p->splits = 1;

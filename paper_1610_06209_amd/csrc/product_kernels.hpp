@@ -371,6 +371,8 @@ constexpr int workgroups_a_unit(int side, int stages, int type) { return side ==
 // LDS that the compiler put right before their products 851 / 1068; banks covered eight lanes at a time, all loads of a chunk in one step 798 / 1000;
 // scales straight from memory 763; results stored from registers 595 / 228 a quarter of the rows, through LDS 571 / 223; eight waves of 128 x 64
 // 623 (four 574) / 1030 (980).  Lines touched two to four chunks ahead of their loads, to have them in the L2: 632 / 512.
+// 8 bits: 16384 x 8192 x 8192 897 to 958 us, 2.3 to 2.45 POP/s (the library behind torch 975), 16384 x 4096 x 4096 240 (243); the matrix pipe is busy 66 % of the time at 1.7 GHz under its
+// load, and zeros for data take 667: the clock bounds it.
 template <int DIRECTION, int TYPE, int BM, int BN, int WM, int WN, int STAGES, bool ANY, typename Out>
 __global__ void __launch_bounds__(64 * WM * WN, workgroups_a_unit(BM, STAGES, TYPE))
 product_kernel(ProductParams p)
@@ -767,14 +769,14 @@ product_kernel(ProductParams p)
 // Measured, the same weights time after time, which the memory's cache holds / others each time: 24 rows over 8 experts of 8192 x 2048 in bf16 (268 MB) 41 /
 // 56 us, 6.5 / 4.8 TB/s; 64 rows over 32 experts of 4096 x 2048 in 4 bits (143 MB) 22.5 / 32 us, 6.3 / 4.5 TB/s; one row, 16384 x 4096 (36 MB) 8.9 us
 // of which the launch and the way to the first weights are half.  With runs of 64 bytes in turn between the waves and scales a byte at a time: 43, 34, 11.2.
-// Weights with the streaming hint, others each time: 56, 31.7; one row, 8192 x 8192 in 4 bits 11.0 for 9.8.
+// Weights with the streaming hint, others each time: 56, 31.7; one row, 8192 x 8192 in 4 bits 11.0 for 9.8.  8 bits, one row, 16384 x 4096 (67 MB) 13 / 17.4 us, 5.1 / 3.9 TB/s, 16 rows 14.7 / 18.4.
 constexpr int kRunSteps = 4;                              // products of a run, 64 bytes of a row each
 template <int TYPE, int NT>
 struct Run {
     uintx4 w[NT][kRunSteps], x[kRunSteps];
     uintx4 ws[NT], xs;                                    // kMx4: the run's scales of the lane's rows
 };
-// RAW (4 bits): the rows are plain numbers of type Out.  Every workgroup rotates and quantises them for itself, a chunk of 512 a wave, into LDS, while its
+// RAW (4 and 8 bits): the rows are plain numbers of type Out.  Every workgroup rotates and quantises them for itself, a chunk of 512 a wave, into LDS, while its
 // first weights are on their way: no launch and no trip through memory in front of them.  The sums are those of two calls, in the same order.  In us, one
 // launch / two: one row, n = 16384, k = 4096, runs of 4096 10.9 / 12.8; n = 4096, k = 2048 5.4 / 5.9; four rows, n = k = 1024 4.3 / 5.2; one row,
 // n = k = 256 3.2 / 4.6.  With four waves that take two chunks each 13.2, four each (two rows) 17.7.
@@ -1087,20 +1089,21 @@ bool whole_pieces(const ProductParams& p)
 
 // Weights' rows a workgroup: more of them share the rows of `a`, fewer leave more workgroups.  16 / 32 / 64, in us: 4 bits, 1 row, n = 8192,
 // k = 8192 8.8 / 9.9 / 13.7; 16 rows, n = 16384, k = 4096 11.9 / 10.2 / 9.8; 64 rows of 32 experts, n = 4096, k = 2048 26.3 / 22.9 / 22.5;
-// bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7
+// bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7; 8 bits, k = 4096, 16 rows, n = 4096 6.7 / 8.3, 6144 9.6 / 8.0, 16384
+// 18.0 / 14.7 (weights that no cache holds 19.2 / 18.4), 5 rows, n = 12288 11.0 / 12.2; 64 rows of 32 experts, n = 4096, k = 2048 45.4 / 42.5 (49.0 / 51.6)
 template <int TYPE, typename Out, bool RAW>
 hipError_t launch_few_rows_as(const ProductParams& p, const RawRows& raw, hipStream_t s)
 {
     const long long sixteens = (p.width + 15) / 16 * (long long)(p.experts < p.rows ? p.experts : p.rows);
     if constexpr (RAW) {
         // (columns for two groups of waves, every workgroup quantises)  16 / 32, in us, bf16: one row, k = 4096, n = 8192 5.85 / 8.1, n = 16384 9.3 / 10.2, 32768 17.2 / 14.2,
-        // 65536 28.4 / 27.0; k = 2048, n = 32768 11.4 / 9.1; four rows, k = 1024, n = 65536 15.3 / 12.3
+        // 65536 28.4 / 27.0; k = 2048, n = 32768 11.4 / 9.1; four rows, k = 1024, n = 65536 15.3 / 12.3; 8 bits, one row, k = 4096, n = 8192 9.3 / 12.7, 16384 13.3 / 14.4, 32768 23.1 / 22.7, four rows, k = 1024, n = 65536 17.3 / 16.2
         if (sixteens >= 2048) return launch_few_rows<TYPE, 2, Out, true>(p, raw, s);
         return launch_few_rows<TYPE, 1, Out, true>(p, raw, s);
     } else {
         if constexpr (TYPE == kMx4)
             if (sixteens >= 4096) return launch_few_rows<TYPE, 4, Out, false>(p, raw, s);
-        if (sixteens >= 1024) return launch_few_rows<TYPE, 2, Out, false>(p, raw, s);
+        if (sixteens >= (TYPE == kInt8 && p.rows > 8LL * p.experts ? 320 : 1024)) return launch_few_rows<TYPE, 2, Out, false>(p, raw, s);
         return launch_few_rows<TYPE, 1, Out, false>(p, raw, s);
     }
 }

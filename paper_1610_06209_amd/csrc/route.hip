@@ -10,7 +10,10 @@ namespace spinner {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFewRouteRows = 2048, kFewEntries = 512;
+// Rows up to which a router takes 64 lanes a row, and from which four (up to kFewChoices choices, and more).  us, 8 of 64 / 256 experts, bf16: 64 and 16 lanes, 2048 rows 3.9 and 4.0 / 4.3 and 4.6,
+// with a bias 5.6 and 6.6 / 6.4 and 7.9, 4096 rows 4.8 and 4.1 / 5.3 and 4.7, biased 7.0 and 6.7 / 7.8 and 7.8.  16 and four lanes, 4 of 32 experts, 8192 rows 3.9 and 3.7, biased 6.8 and 7.4, 16384 4.6
+// and 3.7, 8.5 and 8.0, 131072 18 and 7.3, 41 and 16; 8 of 64, 16384 rows 5.1 and 4.7, biased 8.6 and 11.2, 32768 7.7 and 5.3, 14.8 and 12.5.
+constexpr int kFewRouteRows = 2048, kManyRouteRows = 16384, kFewChoices = 4;
 constexpr long long kRouteBlocks = 1 << 20;          // most workgroups: a grid holds fewer than 2^32 threads, and goes down the rows
 
 // v of the lane that takes turns with this one in a join over 2 MASK lanes, when lanes of MASK have joined before: mirrored rows for 4 and 8, which the
@@ -291,8 +294,10 @@ __device__ __forceinline__ void choose64(const RouteParams& p, const float* l, c
 // LANES lanes a row, up to R neighbouring experts each, in registers from the logits to the choice.
 // A candidate is the largest of whole numbers of 32 bits below the last one: the first 22 (21) of the key's bits in the order of the numbers, and its place
 // in the row's lanes, which puts equal ones in the order of their index.  EXACT (16-bit logits, no bias: the key is the logit, of which 19 bits are all there is): the candidates
-// are the choices.  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32; where those
+// are the choices (16384 x 256, 8 choices: 7.2 us).  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32; where those
 // lie too near each other (and are not equal by having the same logit and bias) by their keys in fp64, and so are groups at the border.
+// The vector ALU bounds it where rows are many: 16383 x 256 bf16, biased sigmoid, groups, 17 us (0.5 TB/s of logits); 65536 x 64 bf16, no bias, 2 choices, 6.9 us (1.2); 8191 x 999 fp32, biased softmax, 11
+// choices, 28 us (1.2).  A round of the choice is two instructions an expert.
 template <typename T, int LANES, int R, int SCORE, bool EXACT>
 __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteParams p)
 {
@@ -329,7 +334,8 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
     }
     // Keys of fp32 that lie nearer may be the other way round.  A sigmoid is off by 4e-7 of itself, its key by 6e-8 more; a softmax by what its sum is off
     // too, (R + 6) 2^-24, which two scores share.
-    const auto reach = [&](float key) { return (SCORE == kSigmoid ? 1.2e-6f : 5e-6f) * (__builtin_fabsf(key) + largest_bias); };
+    // Scores below e^-64 are off by more, where logits that far from the largest are: by less than 1e-32 in all.
+    const auto reach = [&](float key) { return __builtin_fmaf(SCORE == kSigmoid ? 1.2e-6f : 5e-6f, __builtin_fabsf(key) + largest_bias, 1e-32f); };
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
         const long long own = r0 + slot, row = own < p.rows ? own : p.rows - 1;
         float l[R];
@@ -410,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             stays = larger < p.top_groups;
             // the border lies behind the last group that stays
             near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) &
-                   (mine - below <= ((careful || SCORE == kSoftmax) ? 1.2e-5f : 5e-6f) * (__builtin_fabsf(mine) + largest_bias));
+                   (mine - below <= __builtin_fmaf((careful || SCORE == kSoftmax) ? 1.2e-5f : 5e-6f, __builtin_fabsf(mine) + largest_bias, 2e-32f));
             wave_meets();
             if (__builtin_expect(__ballot(near) != 0, 0)) stays = stays64<LANES, SCORE>(p, logits[slot] + lane * R, at, lane, group_keys[slot]);
             near = false;
@@ -440,10 +446,10 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             if constexpr (EXACT) {
                 if (count == p.top) break;
             } else if (count >= p.top) {
-                // (off by 2^-12 of the number, or 2^-138)
+                // (off by 2^-12 of the number, or 2^-138, and by what the scores in few instructions are)
                 const float v = number_of(last & ~kLow);
                 if (count == p.top) border = v;
-                else open = open & (last != 0) & (border - v <= reach(border) + 5e-4f * __builtin_fabsf(border) + 1e-40f);
+                else open = open & (last != 0) & (border - v <= 3.0f * reach(border) + 5e-4f * __builtin_fabsf(border));
                 if (count > p.top && __ballot(open) == 0) break;
                 if (count == CANDIDATES) break;
             }
@@ -579,6 +585,7 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
 //   sigmoid      dl_i = d_i p_i (1 - p_i)
 // and w_j = scale q_j, q_j = p_j / (sum of the chosen ones'), on the chosen ones only
 //   softmax      dl_i = q_i (d_i - sum_j d_j q_j)          sigmoid: (1 - p_i) times that
+// Few numbers are read but for the whole softmax; what it writes bounds it, and the launch: 65536 x 64 bf16 6.5 us (8.4 MB written), 8191 x 999 fp32 10.2 (33 MB, 3.2 TB/s).
 template <typename T, int LANES, int R, int SCORE>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
 {
@@ -696,8 +703,8 @@ hipError_t route_rows(const RouteParams& p, bool grad, hipStream_t s)
 {
     return p.score == kSoftmax ? route_scores<T, LANES, R, kSoftmax>(p, grad, s) : route_scores<T, LANES, R, kSigmoid>(p, grad, s);
 }
-// Lanes a row and experts a lane: four lanes where their registers hold the row, 16 rows a wave, then 16, but 64 for so few rows that waves are to spare;
-// groups have whole lanes of their own.
+// Lanes a row and experts a lane: four lanes where their registers hold the row and there are many, 16 rows a wave, then 16, but 64 for so few rows that waves are
+// to spare; groups have whole lanes of their own.
 template <typename T>
 hipError_t route_any(RouteParams p, bool grad, hipStream_t s)
 {
@@ -710,7 +717,7 @@ hipError_t route_any(RouteParams p, bool grad, hipStream_t s)
         if (many <= 1) return route_rows<T, 64, 1>(p, grad, s);
         if (many <= 4) return route_rows<T, 64, 4>(p, grad, s);
     }
-    if (p.rows > kFewRouteRows) {
+    if (p.rows >= (p.top <= kFewChoices ? kManyRouteRows : 2 * kManyRouteRows)) {
         if (least <= 8) return route_rows<T, 4, 8>(p, grad, s);
         if (least <= 16) return route_rows<T, 4, 16>(p, grad, s);
     }
@@ -734,7 +741,10 @@ hipError_t route(const RouteParams& p, int dtype, bool grad, hipStream_t s)
 // ------------------------------------------------------------------ order
 // Counting sort, stable: an entry's place is the number of entries of smaller experts, and of its own in front of it.  Each workgroup has a run
 // of entries, each of its 16 waves a run of that; entries of no expert count as one expert more.
+// Two launches in a row and reads that wait for each other bound it: one workgroup of 1024 threads 4.0 us for 8 entries, 5.3 for 4096, 8.2 for 8192, 14 for 16384, where several take 8.7 (64 experts).
 constexpr int kOrderThreads = 1024, kHeld = 4;
+// Entries that 256 threads order, which meet sooner (64 experts, us: 8 entries 3.5, with 1024 threads 4.0; 512 3.8, 4.1; 1024 4.3, 4.2).
+constexpr int kFewEntries = 512;
 // Threads of the kernel that orders and the most experts that it has room for in LDS.
 constexpr int kFewExperts = 256;
 constexpr int order_threads(int count) { return count <= kFewExperts ? 1024 : 512; }
@@ -915,8 +925,9 @@ hipError_t launch_route_grad(const RouteParams& p, int dtype, hipStream_t s) { r
 
 void plan_order(OrderParams* p)
 {
-    // one workgroup for few entries (no second launch); otherwise up to 256 of at least as many entries as lie in registers
-    if (p->entries <= 8192) {
+    // one workgroup for few entries (no second launch; 999 experts, one / several: 4096 entries 7.9 / 8.9 us, 8192 12.8 / 9.1); otherwise up to 256 of at least
+    // as many entries as lie in registers
+    if (p->entries <= 2 * kHeld * order_threads(p->count)) {
         p->blocks = 1;
         p->share = p->entries;
         return;

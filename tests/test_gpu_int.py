@@ -110,6 +110,42 @@ def test_rounding_after_a_rotation(gpu, name, k, block):
         assert np.abs(whole(codes, k)).max() == 127
 
 
+MANY = [(5000, 0), (4112, 0), (7680, 32), (8192, 64), (4608, 128), (4352, 256), (5120, 512), (6144, 1024), (8192, 2048), (8192, 4096), (1536, 512), (400, 0), (18432, 1024)]
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("k,block", MANY)
+def test_many_rows_have_the_bits_of_few(gpu, name, k, block):
+    """Rows a workgroup takes in turn, and the forms that only many rows take: codes and scales as of a few rows at a time."""
+    say("int many rows", name, k, block)
+    t = gpu.torch
+    rows = 9001
+    g = t.Generator(device=gpu.dev).manual_seed(k)
+    x = (t.randn((rows, k), device=gpu.dev, generator=g) * t.exp(t.randn((rows, 1), device=gpu.dev, generator=g))).to(gpu.types[name])
+    d = t.sign(t.randn(k, device=gpu.dev, generator=g)) if block else None
+    codes, scales = gpu.b.spinner_int_quantize(x, d, block)
+    for r0 in (0, 500, 1020, 2000, 4093, 8190, rows - 30):
+        c, s = gpu.b.spinner_int_quantize(x[r0:r0 + 30].contiguous(), d, block)
+        assert t.equal(codes[r0:r0 + 30], c) and t.equal(scales[r0:r0 + 30], s), r0
+    # all of them against the number that they stand for: rotated twice is what went in
+    y = gpu.b.spinner_int_dequantize(codes, scales, t.float32, k).double()
+    v = x.double()
+    if block:
+        size = 1
+        v = (v * d.double()).view(rows, -1, block)
+        while size < block:
+            v = v.view(rows, -1, 2, size)
+            v = t.stack((v[:, :, 0] + v[:, :, 1], v[:, :, 0] - v[:, :, 1]), 2)
+            size *= 2
+        v = v.reshape(rows, k) / block ** 0.5
+        norm = (x.double() ** 2).view(rows, -1, block).sum(-1).sqrt().amax(-1, keepdim=True)
+        off = (np.log2(block) + 3) * 2.0 ** -24 * norm
+    else:
+        off = 0.0
+    s = scales.double()[:, None]
+    assert bool(((y - v).abs() <= s * (0.5 + 3e-5) + off + y.abs() * 2.0 ** -24).all())
+
+
 @pytest.mark.parametrize("k,block", [(70, 0), (512, 256), (4096, 4096), (4100, 0), (20480, 2048)])
 def test_rows_to_their_places(gpu, k, block):
     """Codes and scales at their places have the bits of those without, from strided rows and repeated ones too; places outside are passed over."""
@@ -150,7 +186,7 @@ def ragged(rng, rows, experts, spare=0):
 
 
 PRODUCTS = [(1, 16, 1, 1), (1, 4096, 100, 2), (5, 33, 7, 2), (16, 100, 129, 1), (24, 256, 129, 8), (17, 17, 33, 1), (40, 72, 64, 3), (64, 1000, 200, 1), (100, 33, 7, 5),
-            (130, 640, 128, 2), (200, 1000, 130, 64), (257, 2048, 256, 1), (500, 100, 60, 65), (700, 1290, 257, 4), (900, 5000, 264, 3), (4100, 700, 1100, 1), (17000, 300, 520, 3)]
+            (130, 640, 128, 2), (200, 1000, 130, 64), (257, 2048, 256, 1), (500, 100, 60, 65), (700, 1290, 257, 4), (900, 5000, 264, 3), (4100, 700, 1100, 1), (17000, 300, 520, 3), (1500, 2000, 1500, 1), (1300, 300, 2900, 1), (16, 40, 5200, 1), (20, 50, 5111, 2), (7, 24, 17000, 1)]
 
 
 @pytest.mark.parametrize("rows,k,n,experts", PRODUCTS)
@@ -190,7 +226,7 @@ def test_deepest_sums(gpu):
 
 
 LAYERS = [(1, 4096, 300, 1, 4096), (1, 100, 33, 1, 0), (2, 2048, 64, 1, 256), (8, 512, 200, 1, 512), (3, 1001, 40, 1, 0), (1, 4096, 2100, 2, 1024), (8, 480, 130, 4, 32), (7, 512, 96, 9, 0),
-          (37, 1000, 100, 1, 0), (100, 768, 300, 3, 256), (300, 2048, 520, 4, 2048)]
+          (37, 1000, 100, 1, 0), (100, 768, 300, 3, 256), (300, 2048, 520, 4, 2048), (1, 64, 33000, 1, 32), (3, 500, 32800, 1, 0)]
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16", "f16"])

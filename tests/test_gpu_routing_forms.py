@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 # rows, experts, choices, groups, groups that stay: four lanes a row (8 and 16 experts each), 16 lanes (1, 4, 8, 16), 64 (1, 4, 8, 16, 32)
 FORMS = [(2300, 7, 3, 1, 1), (2049, 32, 8, 1, 1), (2100, 61, 5, 1, 1), (2100, 64, 8, 4, 2), (2060, 48, 2, 3, 1), (2050, 40, 9, 1, 1), (2050, 16, 16, 1, 1), (2070, 13, 12, 1, 1), (2050, 100, 8, 4, 3),
          (2050, 128, 10, 8, 4), (2050, 256, 6, 16, 5), (2050, 250, 20, 10, 7), (33, 60, 4, 1, 1), (33, 64, 4, 64, 10), (20, 200, 7, 5, 2), (20, 400, 7, 50, 9), (20, 999, 9, 3, 2), (9, 1000, 30, 40, 25),
-         (2050, 320, 4, 64, 6)]
+         (2050, 320, 4, 64, 6), (16390, 7, 3, 1, 1), (16384, 30, 4, 1, 1), (16385, 64, 4, 4, 2), (32770, 32, 8, 1, 1), (32768, 61, 5, 1, 1), (33000, 64, 8, 4, 3), (32800, 48, 6, 3, 2)]
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
@@ -37,7 +37,7 @@ def test_each_form(gpu, name, case):
         check_grad(numbers(got)[some], ex.route_grad(de[some], xe[some], want_e, score, renormalise), de[some], xe, count, 1.0, name)
 
 
-@pytest.mark.parametrize("rows", [25, 2100])
+@pytest.mark.parametrize("rows", [25, 2100, 33000])
 @pytest.mark.parametrize("count,top", [(24, 8), (64, 8), (200, 12), (1000, 32)])
 def test_keys_level_with_each_other(gpu, rows, count, top):
     """All equal, a few values only, and so near that fp32 does not tell them apart: more of them than a row's candidates; ties by index."""
@@ -75,6 +75,27 @@ def test_scores_too_small_for_32_bits(gpu):
                 want_w, want_e = ex.route(xe, 5, bx, None, score, **groups)
                 assert np.array_equal(numbers(e), want_e), (score, groups)
                 check_weights(numbers(w), want_w, xe, 64)
+
+
+@pytest.mark.parametrize("rows", [400, 5000, 33000])
+@pytest.mark.parametrize("far", [40.0, 66.0, 74.0, 87.3])
+def test_scores_far_below_the_largest(gpu, rows, far):
+    """One logit `far` above all others, which differ by a few places, and biases as small as their scores are: what fp32 rounds there decides nothing."""
+    say("route far", rows, far)
+    rng = np.random.default_rng(int(far) + rows)
+    count, top = 64, 8
+    x = -0.1 + rng.integers(0, 2000, (rows, count)) * 2.0 ** -27
+    x[np.arange(rows), rng.integers(0, count, rows)] = far
+    x, xe = held(gpu, x)
+    some = np.unique(np.concatenate((np.arange(200), rng.integers(0, rows, 200))))
+    small = np.exp(-far - 0.1)
+    for bias in (np.zeros(count), rng.random(count) * small * 1e-5, -small * (1 + 1e-5 * rng.random(count))):
+        b, be = held(gpu, bias)
+        for groups in ({}, dict(groups=4, top_groups=2, group_top=2), dict(groups=4, top_groups=2, group_top=1)):
+            w, e = gpu.b.spinner_route(x, top, b, None, "softmax", **groups)
+            want_w, want_e = ex.route(xe[some], top, be, None, "softmax", **groups)
+            assert np.array_equal(numbers(e)[some], want_e), groups
+            check_weights(numbers(w)[some], want_w, xe, count)
 
 
 def test_rows_beyond_32_bits(gpu):
