@@ -639,7 +639,7 @@ int spinner_route_order(const int *chosen, long count, int experts, int *places,
  * dispatch's out or of dy that no place names is left as it was, one that several
  * name holds parts of any of theirs.  In spinner_combine what has the weight 0 adds nothing,
  * whatever its row holds.  1 <= n <= 2^24, 1 <= top <= 32, rows * top <= 2^31 - 2^16,
- * strides >= 0 (results: >= n) elements.
+ * strides >= 0 (results: >= n) elements.  Results must not overlap what is read.
  */
 int spinner_dispatch(const void *x, int dtype, long rows, int n, long x_stride, const int *places, int top,
                      void *out, long out_stride, void *stream);
