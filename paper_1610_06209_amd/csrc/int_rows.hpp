@@ -24,6 +24,8 @@ hipError_t launch_int_quantize(const IntQuantizeParams& p, int dtype, hipStream_
 hipError_t launch_int_dequantize(const int8_t* codes, const float* scales, int rows, int k, void* out, int dtype, long long out_stride, hipStream_t s);
 
 void plan_product_int(ProductParams* p);
+// weights' rows that a workgroup of the form for few rows takes: 16, 32 or 64; *us: about what that form takes
+int few_columns_int(const ProductParams& p, double* us);
 hipError_t launch_product_int(int out_type, const ProductParams& p, hipStream_t s);           // kForward
 // rows that the product's kernel quantises for itself
 bool int_quantises_within(const ProductParams& p);

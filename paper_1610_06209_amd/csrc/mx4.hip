@@ -155,7 +155,7 @@ constexpr int kHeldDepth = 8192;
 constexpr size_t kMostPartial = 64u << 20;       // bytes of partial sums
 
 template <int N>
-static void shortest(const Form (&forms)[N], int direction, int chunk_numbers, ProductParams* p)
+static double shortest(const Form (&forms)[N], int direction, int chunk_numbers, ProductParams* p)
 {
     const bool mx4 = chunk_numbers == 256;
     double best = 1e30;
@@ -188,6 +188,7 @@ static void shortest(const Form (&forms)[N], int direction, int chunk_numbers, P
             }
         }
     }
+    return best;
 }
 
 // (16-bit rows that are no whole pieces of 16 bytes go by the same choice, though their kernels, 64 x 64 or 128 x 128 and a chunk ahead through registers, take longer: see
@@ -210,13 +211,40 @@ void plan_product(int direction, bool mx4, ProductParams* p)
     else shortest(kForms16, direction, 64, p);
 }
 
-// (A chunk of 128 whole numbers takes the loads, reads and products of one of 64 numbers of 16 bits.)  8 bits, k = n = 4096, us for 100 / 300 / 1000 / 2000 / 16384 (8 experts) rows: 256 x 256 44 / 45 / 47 / 48 /
+// 8-bit whole numbers: a chunk is 128 of them, and takes the loads, reads and products of one of 64 numbers of 16 bits.  k = n = 4096, us for 100 / 300 / 1000 / 2000 / 16384 (8 experts) rows: 256 x 256 44 / 45 / 47 / 48 /
 // 253, 128 x 128 25 / 25 / 27 / 39 / 331, with four chunks in LDS 19 / 20 / 24 / 43 / 361, 64 x 64 11 / 16 / 32 / 60 / 507; n = 16384 with 16 / 17 rows 64 x 64 18.5 / 18.5, few rows 18.5 / 25.7
+constexpr Form kForms8[] = {kForms16[0], kForms16[1], kForms16[2], {kTile64, 64, 0.18, 0.33, 4.4, 512}};
+
+// The form for few rows, 16, 32 or 64 of the weights' rows a workgroup: time of a chunk, in as many rounds as workgroups of 16 rows need, or the weights' way from memory.
+// 16 / 32 / 64, 64 x 64 tiles, us, k = 8192: 4 rows, n = 4096 8.9 / 12.2 / 19.1, 17.5, 5000 14.1 / 12.9 / 19.6, 21.0, 12288 20.5 / 23.0 / 22.2, 24.4; 16 rows, 4096 10.7 / 13.9 / 20.9, 18.1, 8192
+// 18.6 / 15.7 / 21.7, 22.7; 32 rows, 2048 10.6 / 13.8 / 20.8, 16.1, 4096 17.7 / 14.6 / 21.3, 18.3, 8192 32 / 26 / 23, 23; 100 rows, 2048 31 / 25 / 23, 16.3; k = 512: 100 rows, 2048 5.2 / 5.1 / 5.0, 5.4,
+// 4096 6.8 / 6.7 / 6.5, 5.5
+int few_columns_int(const ProductParams& p, double* us)
+{
+    const bool scarce = p.rows <= 8LL * p.experts;
+    const double chunk[] = {scarce ? 0.1 : 0.12, scarce ? 0.155 : 0.173, 0.3}, around[] = {2.7, 3.0, 3.2}, groups = p.experts < p.rows ? p.experts : p.rows;
+    const double tiles = p.experts > 1 ? p.rows / 16.0 + 0.5 * groups : (p.rows + 15) / 16, memory = groups * p.width * p.depth / 5.5e6;
+    int columns = 16;
+    *us = 1e30;
+    for (int i = 0; i < 3; ++i) {
+        const int each = 16 << i;
+        const double work = ceil((double)p.depth / 128) * chunk[i] * ceil(tiles * ((p.width + each - 1) / each) / 256), t = around[i] + (work > memory ? work : memory);
+        if (t < *us) {
+            *us = t;
+            columns = each;
+        }
+    }
+    return columns;
+}
+
 void plan_product_int(ProductParams* p)
 {
     p->splits = 1;
-    if ((p->rows + p->experts - 1) / p->experts <= 16) p->tile = kFewRows;
-    else shortest(kForms16, kForward, 128, p);
+    p->tile = kFewRows;
+    if ((p->rows + p->experts - 1) / p->experts <= 16) return;
+    double few;
+    few_columns_int(*p, &few);
+    if (shortest(kForms8, kForward, 128, p) > few) p->tile = kFewRows;
 }
 
 bool int_quantises_within(const ProductParams& p) { return quantises_within(p); }

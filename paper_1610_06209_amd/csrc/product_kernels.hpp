@@ -1089,8 +1089,7 @@ bool whole_pieces(const ProductParams& p)
 
 // Weights' rows a workgroup: more of them share the rows of `a`, fewer leave more workgroups.  16 / 32 / 64, in us: 4 bits, 1 row, n = 8192,
 // k = 8192 8.8 / 9.9 / 13.7; 16 rows, n = 16384, k = 4096 11.9 / 10.2 / 9.8; 64 rows of 32 experts, n = 4096, k = 2048 26.3 / 22.9 / 22.5;
-// bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7; 8 bits, k = 4096, 16 rows, n = 4096 6.7 / 8.3, 6144 9.6 / 8.0, 16384
-// 18.0 / 14.7 (weights that no cache holds 19.2 / 18.4), 5 rows, n = 12288 11.0 / 12.2; 64 rows of 32 experts, n = 4096, k = 2048 45.4 / 42.5 (49.0 / 51.6)
+// bf16, 16 rows, n = 4096, k = 4096 9.9 / 15.0 / 21.5; 24 rows of 8 experts, n = 8192, k = 2048 42.4 / 41.4 / 47.7; 8 bits: see few_columns_int
 template <int TYPE, typename Out, bool RAW>
 hipError_t launch_few_rows_as(const ProductParams& p, const RawRows& raw, hipStream_t s)
 {
@@ -1103,7 +1102,13 @@ hipError_t launch_few_rows_as(const ProductParams& p, const RawRows& raw, hipStr
     } else {
         if constexpr (TYPE == kMx4)
             if (sixteens >= 4096) return launch_few_rows<TYPE, 4, Out, false>(p, raw, s);
-        if (sixteens >= (TYPE == kInt8 && p.rows > 8LL * p.experts ? 320 : 1024)) return launch_few_rows<TYPE, 2, Out, false>(p, raw, s);
+        if constexpr (TYPE == kInt8) {
+            double us;
+            const int columns = few_columns_int(p, &us);
+            if (columns == 64) return launch_few_rows<TYPE, 4, Out, false>(p, raw, s);
+            return columns == 32 ? launch_few_rows<TYPE, 2, Out, false>(p, raw, s) : launch_few_rows<TYPE, 1, Out, false>(p, raw, s);
+        }
+        if (sixteens >= 1024) return launch_few_rows<TYPE, 2, Out, false>(p, raw, s);
         return launch_few_rows<TYPE, 1, Out, false>(p, raw, s);
     }
 }

@@ -164,3 +164,24 @@ def test_memory_comes_from_the_stream_of_the_call(made, name):
     tensors.clear()
     getattr(binding, name)(**CALLS[name])
     assert tensors and all(t.made_on is CURRENT and not t.used_on for t in tensors)
+
+
+def test_sizes_of_the_products_take_every_form():
+    """The sizes that the 8-bit products are tested at take all of their tiles, and the form for few rows with 16, 32 and 64 columns, by the library's rule."""
+    import ctypes
+
+    import product_forms
+    from paper_1610_06209_amd import binding
+    from test_gpu_int import PRODUCTS
+
+    rule = getattr(binding.lib, "_ZN7spinner16plan_product_intEPNS_13ProductParamsE")
+    columns = getattr(binding.lib, "_ZN7spinner15few_columns_intERKNS_13ProductParamsEPd")
+    rule.restype, columns.restype = None, ctypes.c_int
+    rule.argtypes, columns.argtypes = [ctypes.c_void_p], [ctypes.c_void_p, ctypes.c_void_p]
+    forms = set()
+    for rows, k, n, experts in PRODUCTS:
+        p, us = product_forms._params_class()(rows=rows, experts=experts), ctypes.c_double()
+        p.width, p.depth = n, -(-k // 16) * 16
+        rule(ctypes.addressof(p))
+        forms.add(product_forms.FORMS[p.tile] + (" %d" % columns(ctypes.addressof(p), ctypes.addressof(us)) if p.tile == 0 else ""))
+    assert forms == {"256", "128", "128 deep", "64", "few rows 16", "few rows 32", "few rows 64"}

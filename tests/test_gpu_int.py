@@ -186,7 +186,9 @@ def ragged(rng, rows, experts, spare=0):
 
 
 PRODUCTS = [(1, 16, 1, 1), (1, 4096, 100, 2), (5, 33, 7, 2), (16, 100, 129, 1), (24, 256, 129, 8), (17, 17, 33, 1), (40, 72, 64, 3), (64, 1000, 200, 1), (100, 33, 7, 5),
-            (130, 640, 128, 2), (200, 1000, 130, 64), (257, 2048, 256, 1), (500, 100, 60, 65), (700, 1290, 257, 4), (900, 5000, 264, 3), (4100, 700, 1100, 1), (17000, 300, 520, 3), (1500, 2000, 1500, 1), (1300, 300, 2900, 1), (16, 40, 5200, 1), (20, 50, 5111, 2), (7, 24, 17000, 1)]
+            (130, 640, 128, 2), (200, 1000, 130, 64), (257, 2048, 256, 1), (500, 100, 60, 65), (700, 1290, 257, 4), (900, 5000, 264, 3), (4100, 700, 1100, 1), (17000, 300, 520, 3), (1500, 2000, 1500, 1), (1300, 300, 2900, 1), (16, 40, 5200, 1), (20, 50, 5111, 2), (7, 24, 17000, 1),
+            (70, 1100, 4100, 1), (130, 520, 4500, 2), (300, 72, 4400, 1), (300, 200, 2100, 3), (45, 1500, 6100, 1), (16, 1000, 5000, 1), (20, 700, 5111, 2), (9, 1000, 9000, 1), (64, 1000, 2100, 4),
+            (40, 300, 2500, 2), (320, 100, 3300, 4), (1000, 4100, 70, 3)]
 
 
 @pytest.mark.parametrize("rows,k,n,experts", PRODUCTS)
