@@ -415,8 +415,10 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             }
             stays = larger < p.top_groups;
             // the border lies behind the last group that stays
+            // (a sum of finite keys that left fp32 says nothing)
             near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) &
                    (mine - below <= __builtin_fmaf((careful || SCORE == kSoftmax) ? 1.2e-5f : 5e-6f, __builtin_fabsf(mine) + largest_bias, 2e-32f));
+            near |= (__builtin_fabsf(mine) == INFINITY) & (__builtin_fabsf(two.a) < INFINITY);
             wave_meets();
             if (__builtin_expect(__ballot(near) != 0, 0)) stays = stays64<LANES, SCORE>(p, logits[slot] + lane * R, at, lane, group_keys[slot]);
             near = false;
