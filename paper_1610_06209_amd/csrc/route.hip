@@ -213,6 +213,7 @@ struct Two {
 };
 
 constexpr double kNever = -(double)INFINITY;
+constexpr float kLargest = 3.40282347e38f;
 // most choices of a row of so many lanes, and candidates: its choices and what may lie level with the last of them
 constexpr int most_chosen(int lanes) { return lanes == 4 ? 8 : kMostChosen; }
 constexpr int most_candidates(int lanes) { return lanes == 4 ? 16 : 48; }
@@ -332,10 +333,15 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
         }
         largest_bias = join_lanes<LANES>(largest_bias, Larger{});
     }
-    // Keys of fp32 that lie nearer may be the other way round.  A sigmoid is off by 4e-7 of itself, its key by 6e-8 more; a softmax by what its sum is off
-    // too, (R + 6) 2^-24, which two scores share.
+    // Keys of fp32 that lie nearer may be the other way round.  A sigmoid is off by 4e-7 of itself; a softmax by what its sum is off too, (R + 6) 2^-24, which two
+    // scores share; a score is neither above 1 nor above its key and bias together.  A key is off by half a place of itself more, 6e-8, and so are two.  (A bias
+    // of -1e9 for one expert widens nothing for the others.  Infinite keys are far from finite ones.)
     // Scores below e^-64 are off by more, where logits that far from the largest are: by less than 1e-32 in all.
-    const auto reach = [&](float key) { return __builtin_fmaf(SCORE == kSigmoid ? 1.2e-6f : 5e-6f, __builtin_fabsf(key) + largest_bias, 1e-32f); };
+    const auto size_of = [](float key) { return fminf(__builtin_fabsf(key), kLargest); };
+    const auto reach = [&](float key) {
+        const float size = size_of(key);
+        return __builtin_fmaf(SCORE == kSigmoid ? 1.05e-6f : 4.85e-6f, fminf(size + largest_bias, 1.0f), __builtin_fmaf(1.5e-7f, size, 1e-32f));
+    };
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < p.rows; r0 += (long long)gridDim.x * ROWS) {
         const long long own = r0 + slot, row = own < p.rows ? own : p.rows - 1;
         float l[R];
@@ -405,20 +411,23 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             if ((lane & (each - 1)) == 0) keys[at.group] = mine;
             wave_meets();
             int larger = 0;
-            float below = -INFINITY;       // the largest of the keys that come after this one
 #pragma unroll 4
             for (int g = 0; g < p.groups; ++g) {
                 const float other = keys[g];
-                const bool first = (other > mine) | ((other == mine) & (g < at.group));
-                larger += first ? 1 : 0;
-                below = (first | (g == at.group)) ? below : fmaxf(below, other);
+                larger += ((other > mine) | ((other == mine) & (g < at.group))) ? 1 : 0;
             }
             stays = larger < p.top_groups;
-            // the border lies behind the last group that stays
-            // (a sum of finite keys that left fp32 says nothing)
-            near = scored & (larger == p.top_groups - 1) & (below > -INFINITY) &
-                   (mine - below <= __builtin_fmaf((careful || SCORE == kSoftmax) ? 1.2e-5f : 5e-6f, __builtin_fabsf(mine) + largest_bias, 2e-32f));
-            near |= (__builtin_fabsf(mine) == INFINITY) & (__builtin_fabsf(two.a) < INFINITY);
+            if (scored) {
+                // What a group's key is off by at most: its scores (no more than 1 each), and its keys' and their sum's roundings.  The groups that stay are
+                // the right ones where the least that one of them may be lies above the most that another one may (sums that leave fp32 may be anything beyond).
+                const float first = __builtin_fabsf(two.a), second = p.group_top > 1 && two.b > -INFINITY ? __builtin_fabsf(two.b) : 0.0f;
+                const float score = fminf(__builtin_fmaf((float)p.group_top, largest_bias, first + second), 2.0f);
+                const float round = __builtin_fmaf(2.5e-7f, fminf(first, kLargest), __builtin_fmaf(2.5e-7f, second, 1e-32f));
+                const float off = __builtin_fmaf(SCORE == kSoftmax ? 4.5e-6f + 6e-8f * (R + 6) : careful ? 6e-6f : 2.5e-6f, score, round);
+                const float least = join_lanes<LANES>(stays ? off - fminf(mine, kLargest) : -INFINITY, Larger{});
+                const float most = join_lanes<LANES>(stays || !(two.a > -INFINITY) ? -INFINITY : fmaxf(mine, -kLargest) + off, Larger{});
+                near = (most > -INFINITY) & (most + least >= 0.0f);
+            }
             wave_meets();
             if (__builtin_expect(__ballot(near) != 0, 0)) stays = stays64<LANES, SCORE>(p, logits[slot] + lane * R, at, lane, group_keys[slot]);
             near = false;
@@ -431,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
         }
         // the largest number below the last one, which leaves it the largest of the differences to that, modulo 2^32
         unsigned last = 0xffffffffu;
-        float border = 0.0f;
+        float border = 0.0f;               // what lies clearly below the last choice
         bool open = !EXACT;                // whether there may be more candidates for the last choice
         int count = 0;
         for (;;) {
@@ -450,8 +459,8 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             } else if (count >= p.top) {
                 // (off by 2^-12 of the number, or 2^-138, and by what the scores in few instructions are)
                 const float v = number_of(last & ~kLow);
-                if (count == p.top) border = v;
-                else open = open & (last != 0) & (border - v <= 3.0f * reach(border) + 5e-4f * __builtin_fabsf(border));
+                if (count == p.top) border = v - __builtin_fmaf(3.0f, reach(v), 5e-4f * size_of(v));
+                else open = open & (last != 0) & (v > border);
                 if (count > p.top && __ballot(open) == 0) break;
                 if (count == CANDIDATES) break;
             }

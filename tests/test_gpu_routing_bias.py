@@ -58,3 +58,39 @@ def test_sums_of_two_keys_that_cancel_or_leave_32_bits(gpu, score):
         choices(gpu, x, xe, bias, some, 16, score=score, groups=groups, top_groups=4, group_top=2)
         bias[:24] = 0.1 * rng.standard_normal(24)
         choices(gpu, x, xe, bias, some, 16, score=score, groups=groups, top_groups=4, group_top=2)
+
+
+def test_one_far_bias_does_not_slow_the_others(gpu):
+    """An expert switched off by a large number, or forced by one or by an infinity, costs no more than one of bias -inf: keys that 32 bits tell apart are not taken again."""
+    say("far biases, time")
+    t = gpu.torch
+    g = t.Generator(device=gpu.dev).manual_seed(1)
+    x = (1.5 * t.randn((16384, 256), generator=g, device=gpu.dev)).bfloat16()
+    ordinary = 0.05 * t.randn(256, generator=g, device=gpu.dev)
+
+    def time(bias, o):
+        def call():
+            gpu.b.spinner_route(x, 8, bias, None, "sigmoid", **o)
+        best = 1e9
+        for _ in range(5):
+            a, b = t.cuda.Event(enable_timing=True), t.cuda.Event(enable_timing=True)
+            call()
+            a.record()
+            for _ in range(20):
+                call()
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) / 20)
+        return best
+
+    ratios = {}
+    for o in ({}, dict(groups=8, top_groups=4, group_top=2)):
+        times = {}
+        for far in (-np.inf, -1e9, -1e6, 1e9, np.inf):
+            bias = ordinary.clone()
+            bias[100] = far
+            times[far] = time(bias, o)
+        say("ms", o, {k: round(v, 4) for k, v in times.items()})
+        ratios.update({(len(o), far): times[far] / times[-np.inf] for far in times})
+    # the slow forms take three times as long and more
+    assert max(ratios.values()) < 1.5, ratios
