@@ -563,7 +563,6 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             value[h] = place < 0 ? -INFINITY : logits[slot][place];
             own_top = fmaxf(own_top, SCORE == kSigmoid ? fminf(value[h], 0.0f) : value[h]);
         }
-        float factor = p.scale;
         if (p.renormalise) {
             top = join_lanes<LANES>(own_top, Larger{});
             sum = 0.0f;
@@ -576,14 +575,17 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             if (p.renormalise) sum += value[h];
         }
         if (p.renormalise) sum = join_lanes<LANES>(sum, Sum{});
-        if (p.renormalise || SCORE == kSoftmax) factor = sum > 0.0f ? p.scale / sum : 0.0f;
+        // (quotients, not products with 1 / sum: of one choice the weight is the scale)
+        const bool shared = p.renormalise || SCORE == kSoftmax;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) value[h] = (!shared ? value[h] : sum > 0.0f ? value[h] / sum : 0.0f) * p.scale;
         if (own < p.rows) {
 #pragma unroll
             for (int h = 0; h < HELD; ++h) {
                 const int j = h * LANES + lane;
                 if (j < p.top) {
                     p.experts[own * p.top + j] = routed && !bad ? which[h] : -1;
-                    p.weights[own * p.top + j] = !routed ? 0.0f : bad ? __builtin_nanf("") : value[h] * factor;
+                    p.weights[own * p.top + j] = !routed ? 0.0f : bad ? __builtin_nanf("") : value[h];
                 }
             }
         }
@@ -646,10 +648,11 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
             if (p.renormalise) sum += share[h];
         }
         if (p.renormalise) sum = join_lanes<LANES>(sum, Sum{});
-        const float part = p.renormalise || SCORE == kSoftmax ? (sum > 0.0f ? 1.0f / sum : 0.0f) : 1.0f;
+        // (quotients, not products with 1 / sum: one choice's share is 1, and its gradient 0)
+        const bool shared = p.renormalise || SCORE == kSoftmax;
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
-            share[h] *= part;
+            if (shared) share[h] = sum > 0.0f ? share[h] / sum : 0.0f;
             dot += d[h] * share[h];
         }
         dot = join_lanes<LANES>(dot, Sum{});
@@ -679,7 +682,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
         wave_meets();
         if (own < p.rows) {
             T* to = static_cast<T*>(p.dlogits) + own * p.dstride;
-            const float back = part * dot;
+            const float back = sum > 0.0f ? dot / sum : 0.0f;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 float v[PIECE];
