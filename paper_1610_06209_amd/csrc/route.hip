@@ -701,15 +701,23 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
     }
 }
 
+// The gradient has no groups, whose lanes would hold more experts, and no form of its own for few rows: route_any gives it none of these.
+constexpr bool gradient_takes(int lanes, int r) { return lanes < 64 || r == 8 || r == 16; }
+
 template <typename T, int LANES, int R, int SCORE>
 hipError_t route_scores(const RouteParams& p, bool grad, hipStream_t s)
 {
     constexpr int ROWS = kThreads / LANES;
     const long long want = ((long long)p.rows + ROWS - 1) / ROWS;
     const dim3 blocks((unsigned)(want < kRouteBlocks ? want : kRouteBlocks));
-    if (grad) hipLaunchKernelGGL((route_grad_kernel<T, LANES, R, SCORE>), blocks, dim3(kThreads), 0, s, p);
-    else if (sizeof(T) == 2 && !p.bias) hipLaunchKernelGGL((route_kernel<T, LANES, R, SCORE, sizeof(T) == 2>), blocks, dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((route_kernel<T, LANES, R, SCORE, false>), blocks, dim3(kThreads), 0, s, p);
+    if (grad) {
+        if constexpr (gradient_takes(LANES, R)) hipLaunchKernelGGL((route_grad_kernel<T, LANES, R, SCORE>), blocks, dim3(kThreads), 0, s, p);
+        else return hipErrorInvalidValue;
+    } else if (sizeof(T) == 2 && !p.bias) {
+        hipLaunchKernelGGL((route_kernel<T, LANES, R, SCORE, sizeof(T) == 2>), blocks, dim3(kThreads), 0, s, p);
+    } else {
+        hipLaunchKernelGGL((route_kernel<T, LANES, R, SCORE, false>), blocks, dim3(kThreads), 0, s, p);
+    }
     return hipGetLastError();
 }
 template <typename T, int LANES, int R>
