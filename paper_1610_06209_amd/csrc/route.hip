@@ -331,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
             // (infinities are far from all others)
             largest_bias = fmaxf(largest_bias, __builtin_fabsf(bias[r]) < INFINITY ? __builtin_fabsf(bias[r]) : 0.0f);
         }
-        largest_bias = join_lanes<LANES>(largest_bias, Larger{});
+        // (the same in all rows)
+        largest_bias = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(join_lanes<LANES>(largest_bias, Larger{}))));
     }
     // Keys of fp32 that lie nearer may be the other way round.  A sigmoid is off by 4e-7 of itself; a softmax by what its sum is off too, (R + 6) 2^-24, which two
     // scores share; a score is neither above 1 nor above its key and bias together.  A key is off by half a place of itself more, 6e-8, and so are two.  (A bias
