@@ -54,7 +54,7 @@ struct RunsOfGrid {
     }
 };
 
-// A row is read once and written to each of its places: 16384 x 4 rows of 4096 in bf16, 671 MB, 114 us, 5.9 TB/s.
+// A row is read once and written to each of its places: 16384 x 4 rows of 4096 in bf16, 671 MB, 116 to 126 us, 5.3 to 5.8 TB/s.
 template <int SIZE, int LANES>
 __global__ void __launch_bounds__(kThreads) dispatch_kernel(ExchangeParams p)
 {
@@ -114,7 +114,7 @@ __device__ __forceinline__ void store_piece(T* p, const float* v)
 // out[r] = sum_j w[r][j] y[places[r][j]], fp32, j in order.  What has the weight 0 adds nothing, whatever its row holds: a choice of no expert has it,
 // and its row may never have been written.
 // Four rows on their way at a time (eight are level: 4099 x 6 rows of 1001 in fp16 14.8 us, 14.6).  STREAM: more rows than the memory's cache holds, which then
-// need not keep them: 16384 x 4 rows of 4096 in bf16, 671 MB, 119 us, 5.6 TB/s, for 129; where they would be found there it costs, 19 us for 15.
+// need not keep them: 16384 x 4 rows of 4096 in bf16, 671 MB, 118 us for 127 in turn on one card (104 to 119 on others, 5.6 to 6.4 TB/s); where they would be found there it costs, 19 us for 15.
 template <typename T, int LANES, bool STREAM>
 __global__ void __launch_bounds__(kThreads) combine_kernel(ExchangeParams p)
 {
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(ExchangeParams p)
 }
 
 // dy[places[r][j]] = w[r][j] dout[r], dw[r][j] = sum_i dout[r][i] y[places[r][j]][i]: a workgroup (or LANES of its lanes) a row, a few j at a time
-// 16384 x 4 rows of 4096 in bf16, 1.2 GB, 215 us, 5.6 TB/s (rows read but not written with the streaming hint; without it 223, written with it too 217).
+// 16384 x 4 rows of 4096 in bf16, 1.2 GB, 220 to 230 us, 5.3 to 5.5 TB/s (rows read but not written with the streaming hint: 220 for 228 without it in turn on one card; written with it too level).
 template <typename T, int LANES, bool STREAM>
 __global__ void __launch_bounds__(kThreads) combine_grad_kernel(ExchangeParams p)
 {

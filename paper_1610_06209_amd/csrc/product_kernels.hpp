@@ -371,7 +371,7 @@ constexpr int workgroups_a_unit(int side, int stages, int type) { return side ==
 // LDS that the compiler put right before their products 851 / 1068; banks covered eight lanes at a time, all loads of a chunk in one step 798 / 1000;
 // scales straight from memory 763; results stored from registers 595 / 228 a quarter of the rows, through LDS 571 / 223; eight waves of 128 x 64
 // 623 (four 574) / 1030 (980).  Lines touched two to four chunks ahead of their loads, to have them in the L2: 632 / 512.
-// 8 bits: 16384 x 8192 x 8192 897 to 958 us, 2.3 to 2.45 POP/s (the library behind torch 975), 16384 x 4096 x 4096 240 (243); the matrix pipe is busy 66 % of the time at 1.7 GHz under its
+// 8 bits: 16384 x 8192 x 8192 897 to 963 us, the latter on average, 2.28 to 2.45 POP/s (the library behind torch 975), 16384 x 4096 x 4096 240 (243); the matrix pipe is busy 66 % of the time at 1.7 GHz under its
 // load, and zeros for data take 667: the clock bounds it.
 template <int DIRECTION, int TYPE, int BM, int BN, int WM, int WN, int STAGES, bool ANY, typename Out>
 __global__ void __launch_bounds__(64 * WM * WN, workgroups_a_unit(BM, STAGES, TYPE))
@@ -430,7 +430,7 @@ product_kernel(ProductParams p)
         unsigned tile;
         if (!xcd_run(p.first_block + blockIdx.x, (unsigned)tiles.total * columns, &tile)) return;
         // bands of four row tiles, column by column (8 bits: eight, of which more are of one expert; 16382 uneven rows of 16 experts, 4096 to 4096, bands of
-        // 2 / 4 / 8 / 16 342 / 354 / 336 / 342 us, one weight matrix of 8192 to 8192 967 / 945 / 946 / 972)
+        // 2 / 4 / 8 / 16 342 / 354 / 336 / 342 us in turn on one card, one weight matrix of 8192 to 8192 967 / 945 / 946 / 972)
         constexpr unsigned BAND = INT ? 8 : 4;
         const unsigned band = tile / (BAND * columns), in_band = tile - band * BAND * columns;
         const unsigned height = (unsigned)tiles.total - BAND * band < BAND ? tiles.total - BAND * band : BAND;

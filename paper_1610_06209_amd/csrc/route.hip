@@ -295,10 +295,10 @@ __device__ __forceinline__ void choose64(const RouteParams& p, const float* l, c
 // LANES lanes a row, up to R neighbouring experts each, in registers from the logits to the choice.
 // A candidate is the largest of whole numbers of 32 bits below the last one: the first 22 (21) of the key's bits in the order of the numbers, and its place
 // in the row's lanes, which puts equal ones in the order of their index.  EXACT (16-bit logits, no bias: the key is the logit, of which 19 bits are all there is): the candidates
-// are the choices (16384 x 256, 8 choices: 7.2 us).  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32; where those
+// are the choices (16384 x 256, 8 choices: 6.8 us).  Otherwise candidates are taken until one lies clearly below the last choice, and put in order by their keys in fp32; where those
 // lie too near each other (and are not equal by having the same logit and bias) by their keys in fp64, and so are groups at the border.
-// The vector ALU bounds it where rows are many: 16383 x 256 bf16, biased sigmoid, groups, 17 us (0.5 TB/s of logits); 65536 x 64 bf16, no bias, 2 choices, 6.9 us (1.2); 8191 x 999 fp32, biased softmax, 11
-// choices, 28 us (1.2).  A round of the choice is two instructions an expert.
+// The vector ALU bounds it where rows are many: 16383 x 256 bf16, biased sigmoid, groups, 18 to 20 us (0.45 TB/s of logits); 65536 x 64 bf16, no bias, 2 choices, 5.0 us in a row of launches, 6.4 to 7.0 between
+// others (1.2 to 1.7); 8191 x 999 fp32, biased softmax, 11 choices, 30 us (1.1).  A round of the choice is two instructions an expert.
 template <typename T, int LANES, int R, int SCORE, bool EXACT>
 __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteParams p)
 {
@@ -599,7 +599,8 @@ __global__ void __launch_bounds__(kThreads, R <= 16 ? 4 : 2) route_kernel(RouteP
 //   sigmoid      dl_i = d_i p_i (1 - p_i)
 // and w_j = scale q_j, q_j = p_j / (sum of the chosen ones'), on the chosen ones only
 //   softmax      dl_i = q_i (d_i - sum_j d_j q_j)          sigmoid: (1 - p_i) times that
-// Few numbers are read but for the whole softmax; what it writes bounds it, and the launch: 65536 x 64 bf16 6.5 us (8.4 MB written), 8191 x 999 fp32 10.2 (33 MB, 3.2 TB/s).
+// Few numbers are read but for the whole softmax; what it writes bounds it, and the launch: 65536 x 64 bf16 5.0 us in a row of launches, 6.5 to 7.0 between others (8.4 MB written), 8191 x 999 fp32 10.2 and 10.8
+// (33 MB, 3.0 to 3.2 TB/s).
 template <typename T, int LANES, int R, int SCORE>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteParams p)
 {
